@@ -364,7 +364,7 @@ def _plain_select(st, lohi, bscale):
     box = lohi[page.clamp(min=0)].float().permute(0, 2, 3, 4, 1)               # [seqs, heads, 2, d, width]
     dot = qc.clamp(min=0) @ box[:, :, 1] + qc.clamp(max=0) @ box[:, :, 0]       # whole numbers below 2^24
     sp = bscale[page.clamp(min=0)].permute(0, 2, 1)
-    score = torch.clamp((dot * sq[..., None]) * sp[:, :, None], max=FLT_MAX).amax(dim=2)
+    score = torch.clamp((dot * sq[..., None]) * sp[:, :, None], -FLT_MAX, FLT_MAX).amax(dim=2)
     score = torch.where(torch.isinf(sp), FLT_MAX, score)
     score = torch.where((page < 0)[:, None], -math.inf, score)
     n = ((st["lengths"].long() + c["page"] - 1) // c["page"])[:, None, None]

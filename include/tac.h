@@ -346,6 +346,138 @@ int tac_attend_multi(const tac_attend_job* jobs, int njobs, void* workspace, int
 int tac_attend_multi_static(const tac_attend_job* jobs, int njobs, tac_stream_t stream);
 
 /*
+ * Paged caches: the decode step of a serving batch over record pools (the paper
+ * has no counterpart: it compresses the cache and leaves the serving to a model).
+ *
+ * A pool holds `pages` pages of page_tokens tokens of each of kv_heads heads; the
+ * record slot of (page p, head h, offset o) is (p * kv_heads + h) * page_tokens + o, so
+ * that the records of a page and head lie side by side.  A sequence's token t is in
+ * page table[t / page_tokens] at offset t % page_tokens.  Page tables and lengths are
+ * device memory and are read when the kernels run: a captured CUDA graph sees what
+ * they hold at each replay.
+ *
+ * An entry of a table outside [0, pages) stands for no page: its tokens are treated
+ * as if they were not there.  A length below 0 counts as 0, one above
+ * table_pages * page_tokens as that.  Nothing is read outside the pools.
+ */
+#define TAC_PAGE_TOKENS_MULTIPLE 16   /* page_tokens is a multiple of this, 16..65536 */
+#define TAC_SELECT_MAX_PAGES 262144   /* table_pages of tac_select_pages at most */
+
+typedef struct {
+  const int32_t* table;    /* device: page of (sequence s, column j) at table[s * table_stride + j] */
+  int64_t table_stride;    /* elements, >= table_pages */
+  int32_t table_pages;     /* columns, >= 0 */
+  int32_t seqs;            /* sequences, >= 0 */
+  const int32_t* lengths;  /* device, seqs entries: tokens of each sequence (tac_page_bounds: see start) */
+  int64_t pages;           /* pages of the pools, >= 0 */
+  int32_t kv_heads;        /* >= 1 */
+  int32_t page_tokens;
+} tac_paging;
+
+/*
+ * The box of each (page, head)'s keys, in 8 bits: for every channel j a lower and an
+ * upper bound lo_j 2^e <= k_tj <= hi_j 2^e over the page's keys, lo and hi whole
+ * numbers in [-127, 127], e the page's own exponent.  The keys are those the cache is
+ * encoded from (before D and H), so that  sum_j max(q_j lo_j, q_j hi_j) 2^e  is at
+ * least q . k_t for every key of the page.
+ *   codes   device, 16-byte aligned, int8 [pages][kv_heads][2][d]: lo, then hi
+ *   scales  device, fp32 [pages][kv_heads]: 2^e, or +inf for a page with a key that
+ *           holds a NaN or an infinity (its codes are -127 and 127)
+ */
+typedef struct {
+  int8_t* codes;
+  float* scales;
+  int32_t d;               /* 64 or 128 */
+} tac_page_boxes;
+
+/*
+ * Brings the boxes up to date with keys just written: rows first[s] .. first[s+1] - 1
+ * of k are the keys of sequence s at positions start[s], start[s] + 1, ...  Every
+ * (page, head) they touch gets the box of its earlier tokens and the new ones.  A page
+ * whose offset 0 is among the new rows starts afresh (what the box held is forgotten:
+ * pages are reused).  For a = max |k_tj| of the new rows of a (page, head):
+ *   e' = the smallest whole number >= -126 with a <= 127 * 2^e',  e = max(e of the box, e'),
+ *   lo_j = min(floor(lo_j 2^(e_box - e)), floor(min_t k_tj 2^-e)),  hi_j = max(ceil(..), ceil(..)).
+ * All of it is exact in fp32, and the order of the rows does not matter.
+ *   k      row i, head h at k + (i * row_stride + h * head_stride) elements; dtype TAC_BF16
+ *          or TAC_FP32; rows (the number of rows, >= 0) bounds what is read
+ *   first  device, seqs + 1 entries, or NULL: one row for each sequence (rows == seqs)
+ *   start  device, seqs entries: the position of each sequence's first new row
+ *   paging.lengths is not used and may be NULL.
+ * Rows that fall outside the table, or on no page, are left out.  Two sequences must not
+ * write one page.
+ */
+int tac_page_bounds(const tac_page_boxes* boxes, const tac_paging* paging, const void* k, int32_t dtype, int64_t rows,
+                    int64_t row_stride, int64_t head_stride, const int32_t* first, const int32_t* start,
+                    tac_stream_t stream);
+
+/*
+ * For each (sequence, KV head) the pages that may hold the largest scores of the head's
+ * query group.  Every query a of the group is put in 8 bits with a power of two of its
+ * own, c_aj = round(q_aj 2^-e_a) (halves to even; e_a as above from max |q_aj|; elements
+ * that are not finite count as 0), and page p gets the score
+ *   max_a (sum_j max(c_aj lo_pj, c_aj hi_pj) 2^e_a) 2^e_p, held within +-FLT_MAX,
+ * FLT_MAX where the page's scale is +inf, -inf where the table names no page.  The sums
+ * are whole numbers below 2^24 and the factors powers of two: scores are exact (down to
+ * fp32's smallest number).  Of
+ * the n = ceil(length / page_tokens) pages min(n, budget) are selected: the first
+ * keep_first and the last keep_last, then by score, ties to the lowest index.
+ *   q         head h's group: row a at q + s * seq_stride + (h * group + a) * row_stride (elements)
+ *   selected  device, int32 [seqs][kv_heads][budget]: table columns in ascending order, then -1
+ *   counts    device, int32 [seqs][kv_heads]
+ * 1 <= group <= TAC_MAX_QUERIES; keep_first, keep_last >= 0 with a sum <= budget; budget >= 1.
+ * One launch; no workspace.
+ */
+int tac_select_pages(const tac_page_boxes* boxes, const tac_paging* paging, const void* q, int32_t dtype, int32_t group,
+                     int64_t seq_stride, int64_t row_stride, int32_t budget, int32_t keep_first, int32_t keep_last,
+                     int32_t* selected, int32_t* counts, tac_stream_t stream);
+
+/*
+ * Attention of one new token a sequence over a paged record cache: for each (sequence,
+ * KV head) and query row a of the head's group,
+ *   s_t = scale * (q_a . k^_t),   out_a = sum_t softmax(s)_t v^_t
+ * over the sequence's tokens t, or over those in the pages that `selected` names; k^ and
+ * v^ are the rows tac_decode would produce.  A row with no token gets zeros.
+ *   selected, counts  NULL, or as tac_select_pages writes them (budget entries a (sequence,
+ *           head); entries outside [0, table_pages) are passed over, the order does not
+ *           matter, an entry given twice counts twice; counts outside 0..budget are clamped)
+ *   q, out  head h's group: row a at + s * seq_stride + (h * group + a) * row_stride elements,
+ *           both dtype; 1 <= group <= TAC_MAX_QUERIES
+ *   workspace  device, 16-byte aligned, >= tac_attend_pages_workspace_bytes (its contents need
+ *           no initialisation; calls that share it must not overlap in time)
+ * The tokens of all sequences and heads are dealt evenly to the SMs, which the lengths on
+ * the device decide when the kernel runs; the parts of a (sequence, head) that fall to several
+ * SMs are joined in a fixed order.  Outputs are the same bits for the same call; they may
+ * differ in the last bits between calls of other lengths or batches (the parts fall
+ * elsewhere).  fp32 queries: operands and sums keep fp32's precision.  bf16 queries: k^ and v^
+ * are fp16 numbers times a factor of their record, sums and softmax are fp32.
+ */
+typedef struct {
+  tac_layer_cfg cfg_k, cfg_v;  /* d = 64 or 128, the same for both */
+  const void* k_codes;         /* planes of pages * kv_heads * page_tokens record slots or more */
+  const void* k_norms;
+  const void* v_codes;
+  const void* v_norms;
+  int64_t capacity;            /* record slots of the planes */
+  tac_paging paging;
+  const int32_t* selected;
+  const int32_t* counts;
+  int32_t budget;
+  int32_t dtype;               /* of q and out */
+  int32_t group;
+  float scale;
+  const void* q;
+  int64_t q_seq_stride, q_row_stride;
+  void* out;
+  int64_t out_seq_stride, out_row_stride;
+} tac_attend_pages_args;
+
+/* Workspace bytes (host only; it asks for the current device's SM count).  -1 for a call
+ * that tac_attend_pages would reject. */
+int64_t tac_attend_pages_workspace_bytes(const tac_attend_pages_args* args);
+int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t workspace_bytes, tac_stream_t stream);
+
+/*
  * Transform only, for checking the butterfly: y = H D x (Sec. 2), normalized,
  * written as fp32 rows of d elements (row stride d).  signs: host words as in
  * tac_layer_cfg.signs.  d: any power of two 2..128.

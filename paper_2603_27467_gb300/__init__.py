@@ -7,7 +7,8 @@ built, or no CUDA device is present, calls raise.
 
 Names follow the C ABI: ``make_signs``, ``encode``, ``decode``, ``encode_multi``,
 ``decode_multi``, ``fwht_debug``, plus the plane-geometry and rate helpers
-(Eq. 1 and Eq. 3 of the paper).
+(Eq. 1 and Eq. 3 of the paper).  ``page_bounds``, ``select_pages`` and
+``attend_pages`` serve a cache that lives in pages (``PagedCache``).
 """
 from __future__ import annotations
 
@@ -26,6 +27,7 @@ __all__ = [
     "codes_bytes", "norms_bytes", "avg_angle_bits", "total_bits", "encode", "decode",
     "encode_multi", "decode_multi", "fwht_debug", "last_error", "version", "Cache",
     "AttendJob", "attend_multi", "attend_workspace_bytes",
+    "PagedCache", "PageBounds", "page_bounds", "select_pages", "attend_pages",
 ]
 
 TAC_OK, TAC_E_INVAL, TAC_E_UNSUPPORTED, TAC_E_CUDA, TAC_E_NONFINITE = 0, 1, 2, 3, 4
@@ -130,6 +132,15 @@ def load():
         lib.tac_attend_multi.argtypes = [P(_AttJob), i32, vp, i64, vp]
         lib.tac_attend_multi_static.restype = i32
         lib.tac_attend_multi_static.argtypes = [P(_AttJob), i32, vp]
+        cp = ctypes.c_char_p       # a struct as packed bytes
+        lib.tac_page_bounds.restype = i32
+        lib.tac_page_bounds.argtypes = [cp, cp, vp, i32, i64, i64, i64, vp, vp, vp]
+        lib.tac_select_pages.restype = i32
+        lib.tac_select_pages.argtypes = [cp, cp, vp, i32, i32, i64, i64, i32, i32, i32, vp, vp, vp]
+        lib.tac_attend_pages_workspace_bytes.restype = i64
+        lib.tac_attend_pages_workspace_bytes.argtypes = [cp]
+        lib.tac_attend_pages.restype = i32
+        lib.tac_attend_pages.argtypes = [cp, vp, i64, vp]
         lib.tac_fwht_debug.restype = i32
         lib.tac_fwht_debug.argtypes = [P(_Rows), i32, P(ctypes.c_uint32), vp, vp]
         lib.tac_hw_approx_debug.restype = i32
@@ -596,6 +607,185 @@ def launch_count(jobs) -> int:
         key = (j.cfg.d, str(j.y.dtype), j.cfg.n_angle, j.cfg.norm_bits, j.cfg.norm_mode)
         groups[key] = groups.get(key, 0) + 1
     return sum(-(-c // MAX_JOBS) for c in groups.values())
+
+
+# ---------------------------------------------------------------------------
+# Paged caches (tac_page_bounds, tac_select_pages, tac_attend_pages)
+# ---------------------------------------------------------------------------
+_PAGING_FMT = struct.Struct("=QqiiQqii")
+_BOXES_FMT = struct.Struct("=QQi4x")
+_ATT_PAGES_FMT = struct.Struct("=32s32sQQQQq48sQQiiifQqqQqq")
+
+
+@dataclass
+class PagedCache:
+    """Record pools of one layer: `pages` pages of page_tokens tokens of each KV head.  The
+    record slot of (page p, head h, offset o) is (p * kv_heads + h) * page_tokens + o."""
+    k: Cache
+    v: Cache
+    kv_heads: int
+    page_tokens: int
+
+    def __post_init__(self):
+        if self.k.capacity != self.v.capacity:
+            raise ValueError(f"K and V pools of {self.k.capacity} and {self.v.capacity} record slots")
+
+    @property
+    def pages(self) -> int:
+        return self.k.capacity // (self.kv_heads * self.page_tokens)
+
+    @staticmethod
+    def empty(k_cfg: LayerCfg, v_cfg: LayerCfg, pages: int, kv_heads: int, page_tokens: int, device="cuda") -> "PagedCache":
+        slots = pages * kv_heads * page_tokens
+        return PagedCache(Cache.empty(k_cfg, slots, device), Cache.empty(v_cfg, slots, device), kv_heads, page_tokens)
+
+    def slots(self, page_table, positions, seq=None):
+        """Record slots (int64 [rows * kv_heads], row = token, head) of tokens at `positions` [rows] of the
+        sequences `seq` [rows] (default: one token for each sequence), for EncodeJob.slot."""
+        torch = _torch()
+        pos = positions.long()
+        seq = torch.arange(len(pos), device=pos.device) if seq is None else seq.long()
+        page = page_table[seq, pos // self.page_tokens].long()
+        head = torch.arange(self.kv_heads, device=pos.device)
+        s = (page[:, None] * self.kv_heads + head) * self.page_tokens + (pos % self.page_tokens)[:, None]
+        return s.reshape(-1)
+
+
+@dataclass
+class PageBounds:
+    """The boxes of a paged cache's keys (tac_page_boxes): lo_j 2^e <= k_tj <= hi_j 2^e over each
+    (page, head)'s tokens."""
+    codes: object        # int8 [pages, kv_heads, 2, d]: lo, hi
+    scales: object       # float32 [pages, kv_heads]: 2^e (inf: a key is not finite)
+    page_tokens: int
+
+    @staticmethod
+    def empty(pages: int, kv_heads: int, d: int, page_tokens: int, device="cuda") -> "PageBounds":
+        torch = _torch()
+        return PageBounds(torch.zeros((pages, kv_heads, 2, d), dtype=torch.int8, device=device),
+                          torch.zeros((pages, kv_heads), dtype=torch.float32, device=device), page_tokens)
+
+    def _checked(self):
+        torch = _torch()
+        c, s = self.codes, self.scales
+        if c.dtype != torch.int8 or c.dim() != 4 or c.shape[2] != 2 or not c.is_contiguous() or not c.is_cuda:
+            raise ValueError("bounds.codes: a contiguous int8 [pages, kv_heads, 2, d] device tensor")
+        if s.dtype != torch.float32 or s.shape != c.shape[:2] or not s.is_contiguous() or not s.is_cuda:
+            raise ValueError("bounds.scales: a contiguous float32 [pages, kv_heads] device tensor")
+        return c.shape
+
+
+def _int32(t, shape, name):
+    """Address of a contiguous int32 device tensor of this shape."""
+    torch = _torch()
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name}: a contiguous int32 {list(shape)} device tensor, got {t.dtype} {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _paging_bytes(table, lengths, pages: int, kv_heads: int, page_tokens: int) -> bytes:
+    torch = _torch()
+    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("page_table: an int32 [seqs, pages of a sequence] device tensor with unit inner stride")
+    seqs, width = table.shape
+    stride = table.stride(0) if seqs > 1 else width
+    return _PAGING_FMT.pack(table.data_ptr(), max(stride, width), width, seqs,
+                            0 if lengths is None else _int32(lengths, (seqs,), "lengths"), pages, kv_heads, page_tokens)
+
+
+def _groups(q, seqs: int, kv_heads: int, d: int, name: str):
+    """(address, dtype code, group, sequence stride, row stride) of a [seqs, heads * group, d] tensor."""
+    if q.dim() != 3 or q.shape[0] != seqs or q.shape[2] != d or q.shape[1] % kv_heads or not q.is_cuda or q.stride(2) != 1:
+        raise ValueError(f"{name}: a [{seqs}, query heads (a multiple of {kv_heads}), {d}] device tensor with unit inner "
+                         f"stride, got {tuple(q.shape)}")
+    return q.data_ptr(), _dtype_code(q), q.shape[1] // kv_heads, q.stride(0), q.stride(1)
+
+
+def page_bounds(bounds: PageBounds, k, page_table, start, first=None, stream=None) -> None:
+    """tac_page_bounds: brings the boxes up to date with keys just written.  k [rows, kv_heads, d]
+    (bf16 or fp32): rows first[s] .. first[s + 1] - 1 (first: int32 [seqs + 1]) are the keys of sequence s
+    at positions start[s] (int32 [seqs]) and on; without `first` one row for each sequence."""
+    pages, heads, _, d = bounds._checked()
+    if k.dim() != 3 or k.shape[1] != heads or k.shape[2] != d or not k.is_cuda or k.stride(2) != 1:
+        raise ValueError(f"k: a [rows, {heads}, {d}] device tensor with unit inner stride, got {tuple(k.shape)}")
+    seqs = page_table.shape[0]
+    _check(load().tac_page_bounds(
+        _BOXES_FMT.pack(bounds.codes.data_ptr(), bounds.scales.data_ptr(), d),
+        _paging_bytes(page_table, None, pages, heads, bounds.page_tokens), k.data_ptr(), _dtype_code(k), k.shape[0],
+        k.stride(0), k.stride(1), None if first is None else _int32(first, (seqs + 1,), "first"),
+        _int32(start, (seqs,), "start"), _stream_ptr(stream)))
+
+
+def select_pages(q, bounds: PageBounds, page_table, lengths, budget: int, keep_first: int = 1, keep_last: int = 1,
+                 selected=None, counts=None, stream=None):
+    """tac_select_pages: for each (sequence, KV head) the `budget` pages (table columns) that may hold the
+    largest scores of its queries q [seqs, kv_heads * group, d], the first keep_first and the last keep_last
+    among them.  Returns (selected int32 [seqs, kv_heads, budget], ascending, then -1; counts int32
+    [seqs, kv_heads]), written to `selected` and `counts` where given."""
+    torch = _torch()
+    pages, heads, _, d = bounds._checked()
+    seqs = page_table.shape[0]
+    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q")
+    paging = _paging_bytes(page_table, lengths, pages, heads, bounds.page_tokens)
+    made = []
+    if selected is None:
+        selected = torch.empty((seqs, heads, max(budget, 0)), dtype=torch.int32, device=q.device)
+        made.append(selected)
+    if counts is None:
+        counts = torch.empty((seqs, heads), dtype=torch.int32, device=q.device)
+        made.append(counts)
+    _check(load().tac_select_pages(
+        _BOXES_FMT.pack(bounds.codes.data_ptr(), bounds.scales.data_ptr(), d), paging, ptr, dt, group, s_seq, s_row, budget,
+        keep_first, keep_last, _int32(selected, (seqs, heads, budget), "selected"), _int32(counts, (seqs, heads), "counts"),
+        _stream_ptr(stream)))
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)   # in use on `stream` until its work is done
+    return selected, counts
+
+
+def attend_pages(q, cache: PagedCache, page_table, lengths, scale: float, selected=None, counts=None, out=None,
+                 workspace=None, stream=None):
+    """tac_attend_pages: attention of one new token's queries q [seqs, kv_heads * group, d] (bf16 or fp32) over
+    all tokens of each sequence, or over the pages that select_pages chose (`selected`, `counts`).  Allocates
+    the output and the workspace (torch) where none is given; returns the output."""
+    torch = _torch()
+    heads, d = cache.kv_heads, cache.k.cfg.d
+    seqs = page_table.shape[0]
+    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q")
+    made = []
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made.append(out)
+    o_ptr, o_dt, o_group, o_seq, o_row = _groups(out, seqs, heads, d, "out")
+    if o_dt != dt or o_group != group:
+        raise ValueError("out must match q in shape and dtype")
+    budget, sel_ptr, cnt_ptr = 0, 0, 0
+    if (selected is None) != (counts is None):
+        raise ValueError("selected and counts come together")
+    if selected is not None:
+        if selected.dim() != 3:
+            raise ValueError("selected: an int32 [seqs, kv_heads, budget] tensor")
+        budget = selected.shape[2]
+        sel_ptr = _int32(selected, (seqs, heads, budget), "selected")
+        cnt_ptr = _int32(counts, (seqs, heads), "counts")
+    args = _ATT_PAGES_FMT.pack(
+        _cfg_bytes(cache.k.cfg), _cfg_bytes(cache.v.cfg), cache.k.codes.data_ptr(), cache.k.norms.data_ptr(),
+        cache.v.codes.data_ptr(), cache.v.norms.data_ptr(), cache.k.capacity,
+        _paging_bytes(page_table, lengths, cache.pages, heads, cache.page_tokens), sel_ptr, cnt_ptr, budget, dt, group,
+        scale, ptr, s_seq, s_row, o_ptr, o_seq, o_row)
+    lib = load()
+    if workspace is None:
+        need = lib.tac_attend_pages_workspace_bytes(args)
+        if need < 0:
+            raise TacError(TAC_E_INVAL, last_error())
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        made.append(workspace)
+    _check(lib.tac_attend_pages(args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)   # in use on `stream` until its work is done
+    return out
 
 
 def fwht_debug(x, signs: np.ndarray, d: int, stream=None):

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "tac_attend.cuh"
+#include "tac_pages.cuh"
 
 namespace tac {
 cudaError_t launch_encode_16_bf16(const EncParams& p, int n, int b, int mode, int sms,
@@ -1029,6 +1030,243 @@ int tac_attend_multi_static(const tac_attend_job* jobs, int njobs, tac_stream_t 
   if (num_sms() <= 0) return fail(TAC_E_CUDA, "%s: no CUDA device", who);   // cached for later calls
   if (njobs == 0) return ok();
   return run_attend(jobs, njobs, ws, reinterpret_cast<cudaStream_t>(stream), false, who);
+}
+
+// ---------------------------------------------------------------------------
+// Paged caches
+// ---------------------------------------------------------------------------
+namespace {
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+int check_paging(const tac_paging* g, const char* who, bool lengths) {
+  if (!g) return fail(TAC_E_INVAL, "%s: paging is NULL", who);
+  if (g->seqs < 0 || g->table_pages < 0 || g->pages < 0)
+    return fail(TAC_E_INVAL, "%s: seqs = %d, table_pages = %d, pages = %lld", who, g->seqs, g->table_pages, (long long)g->pages);
+  if (g->kv_heads < 1) return fail(TAC_E_INVAL, "%s: kv_heads = %d", who, g->kv_heads);
+  if (g->page_tokens < TAC_PAGE_TOKENS_MULTIPLE || g->page_tokens > 65536)
+    return fail(TAC_E_INVAL, "%s: page_tokens = %d (%d..65536)", who, g->page_tokens, TAC_PAGE_TOKENS_MULTIPLE);
+  if (g->page_tokens % TAC_PAGE_TOKENS_MULTIPLE)
+    return fail(TAC_E_UNSUPPORTED, "%s: page_tokens = %d is not a multiple of %d", who, g->page_tokens, TAC_PAGE_TOKENS_MULTIPLE);
+  if (g->table_stride < g->table_pages)
+    return fail(TAC_E_INVAL, "%s: table_stride %lld < table_pages %d", who, (long long)g->table_stride, g->table_pages);
+  if (g->seqs > 0 && g->table_pages > 0 && (!g->table || !aligned4(g->table)))
+    return fail(TAC_E_INVAL, "%s: table is NULL or not 4-byte aligned", who);
+  if (lengths && g->seqs > 0 && (!g->lengths || !aligned4(g->lengths)))
+    return fail(TAC_E_INVAL, "%s: lengths is NULL or not 4-byte aligned", who);
+  if ((int64_t)g->table_pages * g->page_tokens > 0x7fffffff)
+    return fail(TAC_E_UNSUPPORTED, "%s: table_pages * page_tokens = %lld is above 2^31 - 1", who,
+                (long long)g->table_pages * g->page_tokens);
+  if ((int64_t)g->seqs * g->kv_heads > (1 << 24))
+    return fail(TAC_E_UNSUPPORTED, "%s: seqs * kv_heads = %lld is above 2^24", who, (long long)g->seqs * g->kv_heads);
+  return TAC_OK;
+}
+
+int check_boxes(const tac_page_boxes* b, const tac_paging* g, const char* who) {
+  if (!b) return fail(TAC_E_INVAL, "%s: boxes is NULL", who);
+  if (b->d != 64 && b->d != 128) return fail(TAC_E_UNSUPPORTED, "%s: d = %d (64, 128)", who, b->d);
+  if (g->pages > 0 && (!b->codes || !aligned16(b->codes) || !b->scales || !aligned4(b->scales)))
+    return fail(TAC_E_INVAL, "%s: boxes.codes or boxes.scales is NULL or misaligned", who);
+  return TAC_OK;
+}
+
+// Rows of `elements` elements at the given strides (elements): 16-byte aligned throughout.
+int check_strided(const void* data, int dtype, int64_t s0, int64_t s1, const char* who, const char* name) {
+  const int esz = esize(dtype);
+  if (!esz) return fail(TAC_E_INVAL, "%s: dtype = %d", who, dtype);
+  if (!data || !aligned16(data)) return fail(TAC_E_INVAL, "%s: %s is NULL or not 16-byte aligned", who, name);
+  if (s0 < 0 || s1 < 0) return fail(TAC_E_INVAL, "%s: %s has a negative stride", who, name);
+  if ((s0 * esz) % 16 || (s1 * esz) % 16)
+    return fail(TAC_E_INVAL, "%s: a stride of %s times sizeof(element) is not a multiple of 16", who, name);
+  return TAC_OK;
+}
+
+tac::Paging to_paging(const tac_paging* g) {
+  tac::Paging o;
+  o.table = g->table;
+  o.lengths = g->lengths;
+  o.table_stride = g->table_stride;
+  o.pages = g->pages;
+  o.width = g->table_pages;
+  o.seqs = g->seqs;
+  o.heads = g->kv_heads;
+  o.page = g->page_tokens;
+  return o;
+}
+
+void to_book(tac::Book* b, const tac_layer_cfg* c, const void* codes, const void* norms, int64_t capacity) {
+  b->codes = static_cast<const uint8_t*>(codes);
+  b->norms = static_cast<const uint8_t*>(norms);
+  b->hdr = b->norms + header_offset(c, capacity);
+  b->n = c->n_angle;
+  b->w = tac::code_bits(c->n_angle);
+  b->nc = tac::att_norm_case(c->norm_bits, c->norm_mode);
+  b->ab = (int32_t)angle_row_bytes(c);
+  b->nb = (int32_t)norm_row_bytes(c);
+  b->hb = c->norm_mode == TAC_NORM_FP32 ? 0 : 8;
+  copy_signs(b->signs, c);
+}
+
+int check_attend_pages(const tac_attend_pages_args* A, const char* who) {
+  if (!A) return fail(TAC_E_INVAL, "%s: args is NULL", who);
+  int rc = check_cfg(&A->cfg_k, who);
+  if (!rc) rc = check_cfg(&A->cfg_v, who);
+  if (!rc) rc = check_paging(&A->paging, who, true);
+  if (rc) return rc;
+  const int d = A->cfg_k.d;
+  if (A->cfg_v.d != d) return fail(TAC_E_INVAL, "%s: K and V d differ (%d, %d)", who, d, A->cfg_v.d);
+  if (d != 64 && d != 128) return fail(TAC_E_UNSUPPORTED, "%s: d = %d (64, 128)", who, d);
+  const tac_paging& g = A->paging;
+  if (A->group < 1 || A->group > TAC_MAX_QUERIES)
+    return fail(TAC_E_INVAL, "%s: group = %d (1..%d)", who, A->group, TAC_MAX_QUERIES);
+  if (!esize(A->dtype)) return fail(TAC_E_INVAL, "%s: dtype = %d", who, A->dtype);
+  if (!(A->scale == A->scale)) return fail(TAC_E_INVAL, "%s: scale is NaN", who);
+  if (A->capacity < 0 || g.pages > A->capacity / ((int64_t)g.kv_heads * g.page_tokens))
+    return fail(TAC_E_INVAL, "%s: %lld pages of %d heads x %d tokens do not fit %lld record slots", who, (long long)g.pages,
+                g.kv_heads, g.page_tokens, (long long)A->capacity);
+  if ((A->selected == nullptr) != (A->counts == nullptr))
+    return fail(TAC_E_INVAL, "%s: selected and counts come together", who);
+  if (A->selected && (A->budget < 1 || !aligned4(A->selected) || !aligned4(A->counts)))
+    return fail(TAC_E_INVAL, "%s: budget = %d, or selected or counts is not 4-byte aligned", who, A->budget);
+  // tiles, their total and the second kernel's grid are 32-bit numbers
+  const int64_t per = g.page_tokens / tac::kTile, segs = (int64_t)g.seqs * g.kv_heads;
+  const int64_t cols = A->selected ? A->budget : g.table_pages;
+  if (cols * per > 0x7fffffff || (segs > 0 && cols * per > 0x7fffffff / segs) || segs * A->group > 0x7fffffff)
+    return fail(TAC_E_UNSUPPORTED, "%s: more than 2^31 - 1 tiles of 16 tokens in one call", who);
+  if (segs == 0) return TAC_OK;
+  if (g.pages > 0 && (!A->k_codes || !A->k_norms || !A->v_codes || !A->v_norms || !aligned16(A->k_codes) ||
+                      !aligned16(A->k_norms) || !aligned16(A->v_codes) || !aligned16(A->v_norms)))
+    return fail(TAC_E_INVAL, "%s: a record plane is NULL or not 16-byte aligned", who);
+  rc = check_strided(A->q, A->dtype, A->q_seq_stride, A->q_row_stride, who, "q");
+  if (!rc) rc = check_strided(A->out, A->dtype, A->out_seq_stride, A->out_row_stride, who, "out");
+  return rc;
+}
+
+// Workspace: the plan (items + 2 words), then the parts of every CTA.
+int attend_pages_items(const tac_attend_pages_args* A) {
+  return A->selected ? A->paging.seqs * A->paging.kv_heads : A->paging.seqs;
+}
+int64_t attend_pages_plan_bytes(const tac_attend_pages_args* A) { return (4 * ((int64_t)attend_pages_items(A) + 2) + 15) & ~(int64_t)15; }
+int64_t attend_pages_bytes(const tac_attend_pages_args* A, int ctas) {
+  return attend_pages_plan_bytes(A) + (int64_t)ctas * 2 * A->group * tac::pg_rec_floats(A->cfg_k.d) * 4;
+}
+
+}  // namespace
+
+int tac_page_bounds(const tac_page_boxes* boxes, const tac_paging* paging, const void* k, int32_t dtype, int64_t rows,
+                    int64_t row_stride, int64_t head_stride, const int32_t* first, const int32_t* start,
+                    tac_stream_t stream) {
+  static const char* who = "tac_page_bounds";
+  int rc = check_paging(paging, who, false);
+  if (!rc) rc = check_boxes(boxes, paging, who);
+  if (rc) return rc;
+  if (!esize(dtype)) return fail(TAC_E_INVAL, "%s: dtype = %d", who, dtype);
+  if (rows < 0 || rows > 0x7fffffff) return fail(TAC_E_INVAL, "%s: rows = %lld", who, (long long)rows);
+  if (!first && rows != paging->seqs)
+    return fail(TAC_E_INVAL, "%s: %lld rows for %d sequences without first", who, (long long)rows, paging->seqs);
+  if (rows == 0 || paging->seqs == 0 || paging->table_pages == 0) return ok();
+  if (!start || !aligned4(start) || !aligned4(first)) return fail(TAC_E_INVAL, "%s: start is NULL, or start or first is not 4-byte aligned", who);
+  rc = check_strided(k, dtype, row_stride, head_stride, who, "k");
+  if (rc) return rc;
+  const int sms = num_sms();
+  if (sms <= 0) return fail(TAC_E_CUDA, "%s: no CUDA device", who);
+  tac::BoundsParams P;
+  P.pg = to_paging(paging);
+  P.codes = boxes->codes;
+  P.scales = boxes->scales;
+  P.k = k;
+  P.rows = rows;
+  P.row_stride = row_stride;
+  P.head_stride = head_stride;
+  P.first = first;
+  P.start = start;
+  const cudaError_t e = tac::launch_page_bounds(boxes->d, dtype, P, sms, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail(TAC_E_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+  return ok();
+}
+
+int tac_select_pages(const tac_page_boxes* boxes, const tac_paging* paging, const void* q, int32_t dtype, int32_t group,
+                     int64_t seq_stride, int64_t row_stride, int32_t budget, int32_t keep_first, int32_t keep_last,
+                     int32_t* selected, int32_t* counts, tac_stream_t stream) {
+  static const char* who = "tac_select_pages";
+  int rc = check_paging(paging, who, true);
+  if (!rc) rc = check_boxes(boxes, paging, who);
+  if (rc) return rc;
+  if (!esize(dtype)) return fail(TAC_E_INVAL, "%s: dtype = %d", who, dtype);
+  if (group < 1 || group > TAC_MAX_QUERIES) return fail(TAC_E_INVAL, "%s: group = %d (1..%d)", who, group, TAC_MAX_QUERIES);
+  if (budget < 1) return fail(TAC_E_INVAL, "%s: budget = %d", who, budget);
+  if (keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > budget)
+    return fail(TAC_E_INVAL, "%s: keep_first %d and keep_last %d with a budget of %d", who, keep_first, keep_last, budget);
+  if (paging->table_pages > TAC_SELECT_MAX_PAGES)
+    return fail(TAC_E_UNSUPPORTED, "%s: table_pages = %d (at most %d)", who, paging->table_pages, TAC_SELECT_MAX_PAGES);
+  if (paging->seqs == 0) return ok();
+  rc = check_strided(q, dtype, seq_stride, row_stride, who, "q");
+  if (rc) return rc;
+  if (!selected || !counts || !aligned4(selected) || !aligned4(counts))
+    return fail(TAC_E_INVAL, "%s: selected or counts is NULL or not 4-byte aligned", who);
+  const int sms = num_sms();
+  if (sms <= 0) return fail(TAC_E_CUDA, "%s: no CUDA device", who);
+  tac::SelectParams P;
+  P.pg = to_paging(paging);
+  P.codes = boxes->codes;
+  P.scales = boxes->scales;
+  P.q = q;
+  P.seq_stride = seq_stride;
+  P.row_stride = row_stride;
+  P.group = group;
+  P.budget = budget;
+  P.keep_first = keep_first;
+  P.keep_last = keep_last;
+  P.selected = selected;
+  P.counts = counts;
+  const cudaError_t e = tac::launch_select_pages(boxes->d, dtype, P, sms, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail(TAC_E_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+  return ok();
+}
+
+int64_t tac_attend_pages_workspace_bytes(const tac_attend_pages_args* args) {
+  static const char* who = "tac_attend_pages_workspace_bytes";
+  if (check_attend_pages(args, who)) return -1;
+  const int sms = num_sms();
+  if (sms <= 0) { fail(TAC_E_CUDA, "%s: no CUDA device", who); return -1; }
+  ok();
+  return attend_pages_bytes(args, tac::attend_pages_ctas(args->cfg_k.d, args->dtype, args->group, sms));
+}
+
+int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t workspace_bytes, tac_stream_t stream) {
+  static const char* who = "tac_attend_pages";
+  const int rc = check_attend_pages(args, who);
+  if (rc) return rc;
+  const tac_paging& g = args->paging;
+  if (g.seqs == 0) return ok();
+  const int sms = num_sms();
+  if (sms <= 0) return fail(TAC_E_CUDA, "%s: no CUDA device", who);
+  const int d = args->cfg_k.d, ctas = tac::attend_pages_ctas(d, args->dtype, args->group, sms);
+  const int64_t need = attend_pages_bytes(args, ctas);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need)
+    return fail(TAC_E_INVAL, "%s: workspace NULL, misaligned or smaller than %lld bytes", who, (long long)need);
+  tac::AttPagesParams P;
+  P.pg = to_paging(&g);
+  to_book(&P.k, &args->cfg_k, args->k_codes, args->k_norms, args->capacity);
+  to_book(&P.v, &args->cfg_v, args->v_codes, args->v_norms, args->capacity);
+  P.selected = args->selected;
+  P.counts = args->counts;
+  P.budget = args->selected ? args->budget : 0;
+  P.group = args->group;
+  P.scale = args->scale;
+  P.q = args->q;
+  P.out = args->out;
+  P.q_seq = args->q_seq_stride;
+  P.q_row = args->q_row_stride;
+  P.o_seq = args->out_seq_stride;
+  P.o_row = args->out_row_stride;
+  P.ctas = ctas;
+  P.items = attend_pages_items(args);
+  P.plan = static_cast<int32_t*>(workspace);
+  P.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attend_pages_plan_bytes(args));
+  const cudaError_t e = tac::launch_attend_pages(d, args->dtype, P, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail(TAC_E_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+  return ok();
 }
 
 int tac_fwht_debug(const tac_rows* x, int d, const uint32_t* signs, float* y, tac_stream_t stream) {

@@ -14,6 +14,8 @@
 #include <algorithm>
 #include <atomic>
 
+#include <cuda_fp16.h>
+
 #include "tac_pages.cuh"
 
 namespace tac {
@@ -24,8 +26,8 @@ struct IC { static constexpr int value = V; };
 constexpr float kPgLog2e = 1.4426950408889634f;
 constexpr int kBatch = 2 * kTile;
 constexpr int kMaxWarps = 16;
-constexpr int kCopies = 16;                       // of each bin-centre table: a half-warp's lookups fall in distinct banks
-constexpr int kTabShift = 7;                      // log2 of an entry's bytes, all copies
+constexpr int kTabShift = 7;                      // log2 of a bin-centre table entry's bytes, all copies
+constexpr float kUnit = 32768.f;                  // fp16 bin centres are scaled by it
 
 // Bin centres (cos, sin)(2 pi k / n) of every supported n, rounded from fp64 by the host compiler.
 namespace cx {
@@ -70,6 +72,28 @@ __device__ __forceinline__ bool pg_bar_wait(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void pg_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ uint32_t pg_rotr(uint32_t x, int s) { return __funnelshift_r(x, x, s); }
 __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+
+__device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ __half2 h2_of(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) { return h2_bits(__hmul2(h2_of(a), h2_of(b))); }
+__device__ __forceinline__ uint32_t hlow2(uint32_t a) { return h2_bits(__low2half2(h2_of(a))); }
+__device__ __forceinline__ uint32_t hhigh2(uint32_t a) { return h2_bits(__high2half2(h2_of(a))); }
+__device__ __forceinline__ uint32_t hex2(uint32_t a) { uint32_t r; asm("ex2.approx.f16x2 %0, %1;" : "=r"(r) : "r"(a)); return r; }
+// A 16-byte load the compiler may not hoist: keeps a loop-invariant operand in shared memory.
+__device__ __forceinline__ uint4 pg_reload(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+// d += a b: one m16n8k16 step, fp16 operands, fp32 accumulators.
+__device__ __forceinline__ void pg_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 2^k, k held within [-126, 126]; the exponent of a nonnegative fp32 number (-127: zero and subnormals).
+__device__ __forceinline__ float pg_exp2i(int k) { return pow2i(min(max(k, -126), 126)); }
+__device__ __forceinline__ int pg_exp_of(float x) { return (int)((__float_as_uint(x) >> 23) & 0xFFu) - 127; }
 
 // Unnormalized Walsh-Hadamard transform of a row of D floats over a warp: lane l holds
 // elements E l .. E l + E - 1, E = D / 32.
@@ -254,23 +278,30 @@ __device__ __forceinline__ bool cursor_next(const AttPagesParams& p, Cursor& c, 
   return true;
 }
 
-// Shared memory of the fp32 kernel.
-template <int D, int QT>
-struct PgF {
+// Shared memory of a warp and the lanes' shares of a record.  EXACT: fp32 products on the CUDA
+// cores (fp32 queries); otherwise fp16 products on the tensor cores.
+template <int D, int QT, bool EXACT>
+struct Pg {
   static constexpr int P = D / 2, NQ = 4 * QT, E = D / 32;
   static constexpr int KP = P / 4;                 // K: positions of a token a lane takes (4 lanes a token)
-  static constexpr int VL = P / 4, VT = 32 / VL;   // V: lanes a token (4 positions each), tokens at a time
-  static constexpr int QRUN = KP * 8 + 16;         // a lane's run of a query: padded, the four runs fall in distinct banks
+  static constexpr int KS = KP / 2;                // K: mma steps of a tile
+  static constexpr int VL = P / 4, VT = 32 / VL;   // V, EXACT: lanes a token (4 positions each), tokens at a time
+  static constexpr int VP = P / 8, MT = P / 16;    // V, mma: positions of a token a lane takes (8 lanes a token), row tiles
+  static constexpr int QRUN = KP * 8 + 16;         // EXACT: a lane's run of a query, padded: the four runs fall in distinct banks
+  static constexpr int QBYTES = EXACT ? NQ * 4 * QRUN : KS * QT * 256;
   static constexpr int REC = NQ * pg_rec_floats(D) * 4;
-  // per warp: rotated queries (and the record of a part that ends here) | record of a part
-  // that began in an earlier warp | constants of the batch's tokens | softmax weights | staging
+  // per warp: rotated queries (and the record of a part that ends here) | record of a part that
+  // began in an earlier warp | the queries' scales | constants of the batch's tokens: K, V, V's
+  // exponent slopes | softmax weights (EXACT) | staging
   static constexpr int W_Q = 0;
-  static constexpr int W_REC = W_Q + NQ * 4 * QRUN;
-  static constexpr int W_KC = W_REC + (REC + 15) / 16 * 16;
+  static constexpr int W_REC = ((QBYTES > REC ? QBYTES : REC) + 15) / 16 * 16;
+  static constexpr int W_QS = W_REC + (REC + 15) / 16 * 16;
+  static constexpr int W_KC = W_QS + NQ * 4;
   static constexpr int W_VC = W_KC + kBatch * 8;
-  static constexpr int W_P = W_VC + kBatch * 8;
-  static constexpr int W_STG = W_P + kBatch * NQ * 4;
-  static_assert(NQ * 4 * QRUN >= REC && W_KC % 16 == 0, "layout");
+  static constexpr int W_VD = W_VC + kBatch * 8;
+  static constexpr int W_P = W_VD + (EXACT ? 0 : kBatch * 4);
+  static constexpr int W_STG = W_P + (EXACT ? kBatch * NQ * 4 : 0);
+  static_assert(W_KC % 16 == 0 && W_STG % 16 == 0, "layout");
 };
 __host__ __device__ inline int pg_stage_bytes(const Book& b) { return kBatch * (b.ab + b.nb + b.hb) + 16; }
 
@@ -425,14 +456,41 @@ __device__ __forceinline__ float pg_norm(const uint32_t* w, int j, float2 ab) {
   }
 }
 
-template <int D, int QT>
+// 2^(log2 r^ - log2 r_max) of two norms as halves.  4-bit codes j and j + 4 of a word become the
+// halves 16 + c (the code in the mantissa's upper bits), one fma with slope and offset from
+// pg_log_consts; 8-bit codes become c - 255, exact.  sl: (slope, offset).
+__device__ __forceinline__ uint32_t pg_log_norm4(uint32_t w, int j, uint32_t slope2, uint32_t offset2) {
+  const uint32_t c = (pg_rotr(w, (4 * j - 6) & 31) & 0x03C003C0u) | 0x4C004C00u;
+  return hex2(h2_bits(__hfma2(h2_of(c), h2_of(slope2), h2_of(offset2))));
+}
+template <int BITS>
+__device__ __forceinline__ uint32_t pg_log_norm(uint32_t w, int j, uint32_t sl) {
+  if constexpr (BITS == 4) {
+    return pg_log_norm4(w, j, hlow2(sl), hhigh2(sl));
+  } else {
+    const uint32_t c = __byte_perm(w, 0x64646464u, j ? 0x4342 : 0x4140);     // 1024 + c
+    return hex2(hmul2(h2_bits(__hsub2(h2_of(c), __float2half2_rn(1279.f))), hlow2(sl)));
+  }
+}
+// (slope, offset) of a record's log2 norms as halves, and the factor outside: r_max, corrected for
+// what rounding the two moved the largest code by.
+__device__ __forceinline__ uint32_t pg_log_consts(float2 h, int nc, float& factor) {
+  const bool spread = h.y > h.x;
+  const float d = spread ? (lg2_approx(h.y) - lg2_approx(h.x)) * (nc == 3 ? 1.f / 255.f : 1.f / 15.f) : 0.f;
+  const __half slope = __float2half_rn(d), off = nc == 3 ? __float2half_rn(0.f) : __float2half_rn(-31.f * __half2float(slope));
+  const float moved = nc == 3 ? 0.f : __fmaf_rn(31.f, __half2float(slope), __half2float(off));
+  factor = h.y * ex2_approx(-moved);
+  return h2_bits(__halves2half2(slope, off));
+}
+
+template <int D, int QT, bool EXACT>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
-    attend_pages_f32(const __grid_constant__ AttPagesParams p, int bf_, int tab_v, int warp_bytes) {
-  using C = PgF<D, QT>;
-  constexpr int P = C::P, NQ = C::NQ, E = C::E, KP = C::KP, VL = C::VL, VT = C::VT;
+    attend_pages_kernel(const __grid_constant__ AttPagesParams p, int tab_v, int warp_bytes) {
+  using C = Pg<D, QT, EXACT>;
+  constexpr int NQ = C::NQ, E = C::E, KP = C::KP, KS = C::KS, VL = C::VL, VT = C::VT, VP = C::VP, MT = C::MT;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ PgShared sh;
-  const bool bf = bf_ != 0;
+  constexpr bool bf = !EXACT;                      // bf16 queries and outputs, else fp32
   const int tid = threadIdx.x, lane = tid & 31, nw = blockDim.x >> 5;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int g = lane >> 2, t = lane & 3;
@@ -448,7 +506,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   uint8_t* const st_vh = st_vn + kBatch * p.v.nb;
   float2* const kc = reinterpret_cast<float2*>(pw + C::W_KC);
   float2* const vc = reinterpret_cast<float2*>(pw + C::W_VC);
-  float* const wt = reinterpret_cast<float*>(pw + C::W_P);       // [token][query]
+  uint32_t* const vd = reinterpret_cast<uint32_t*>(pw + C::W_VD);  // mma: (slope, offset) of V's log2 norms, two halves
+  float* const wt = reinterpret_cast<float*>(pw + C::W_P);       // EXACT: [token][query]
   auto rec_of = [&](int w, int which) {
     return reinterpret_cast<float*>(pool + w * warp_bytes + (which ? C::W_Q : C::W_REC));
   };
@@ -501,21 +560,34 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     issue(true, nx);
   }
 
-  // ---- bin-centre tables: entry k, copy c at k 2^kTabShift + 8 c; entries n .. 2^w - 1 repeat
-  // entry n - 1 (codes >= n count as that) ----
+  // ---- bin-centre tables, every entry 2^kTabShift bytes of copies (EXACT: 16 of two floats, so
+  // that a half-warp's lookups fall in distinct banks; otherwise 32 of two halves, a warp's);
+  // entries n .. 2^w - 1 repeat entry n - 1 (codes >= n count as that) ----
   for (int side = 0; side < (tab_v ? 2 : 1); ++side) {
     const Book& bk = tab_v && side == 0 ? p.k : p.v;
-    float2* const tab = reinterpret_cast<float2*>(side ? tv : tk);
-    for (int e = tid; e < (1 << bk.w) * kCopies; e += blockDim.x)
-      tab[e] = g_pg_centre.v[tab_offset_n(bk.n) + min(e / kCopies, bk.n - 1)];
+    uint4* const tab = reinterpret_cast<uint4*>(side ? tv : tk);
+    for (int e = tid; e < (8 << bk.w); e += blockDim.x) {
+      const float2 c = g_pg_centre.v[tab_offset_n(bk.n) + min(e >> 3, bk.n - 1)];
+      uint32_t x, y;
+      if constexpr (EXACT) {
+        x = __float_as_uint(c.x);
+        y = __float_as_uint(c.y);
+      } else {
+        x = y = h2_bits(__floats2half2_rn(c.x * kUnit, c.y * kUnit));
+      }
+      tab[e] = make_uint4(x, y, x, y);
+    }
   }
   __syncthreads();
 
-  const uint32_t lane_off = (uint32_t)(lane % kCopies) * 8;
+  const uint32_t lane_off = EXACT ? (uint32_t)(lane & 15) * 8 : (uint32_t)lane * 4;
   const uint32_t km = ((1u << p.k.w) - 1u) << kTabShift, vm = ((1u << p.v.w) - 1u) << kTabShift;
   bool begun = false;                              // this warp has the first tile of the current (sequence, head)
   float m_[QT], l_[QT];
-  float2 acc[NQ][4];
+  float2 acc[EXACT ? NQ : 1][4];                   // EXACT: [query][position]
+  float am[EXACT ? 1 : QT][MT][4];                 // mma: [.][row tile]: (cos, sin) of two positions, query 4 x + t
+  int ae[QT];                                      // mma: am is in units of 2^ae / kUnit
+  float qsc[QT];                                   // mma: the scale of query 4 x + t
 
   // Scores of the staged batch: lane (g, t) takes positions KP t .. KP t + KP - 1 of tokens g and
   // g + 8 of a tile.  sv[x][i]: token 16 (i / 2) + 8 (i & 1) + g, query 4 x + t.
@@ -640,6 +712,229 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     }
   };
 
+  // ---- the same on the tensor cores ----
+  // Norms enter a record's products as halves: linear norm codes c as the subnormal half c 2^-24
+  // (its bits are the code), so that r^ u = r_min u + Delta (c u) takes two sums with r_min and Delta
+  // outside, in fp32; log norms as 2^(log2 r^ - log2 r_max) by the hardware's exponential of two halves
+  // (2^-9.9), r_max outside; fp32 norms over the record's power of two.
+  // Rows of the scores' fragments are tokens, steps run over the positions; column 2 a (2 a + 1) is
+  // the fp16 number next to query a's element (what is left of it).
+  auto scores_mma = [&](float (&sv)[QT][4], auto nc_) {
+    constexpr int NC = decltype(nc_)::value;
+    constexpr bool F32N = NC == 4, LIN = NC == 0 || NC == 2;
+    constexpr int KB = NC <= 1 ? 4 : 8, KW = F32N ? 1 : KP * KB / 32;
+    const int wk = p.k.w;
+    const uint32_t qaddr = pg_smem(pw + C::W_Q) + 16 * lane;
+#pragma unroll
+    for (int x = 0; x < QT; ++x) sv[x][2] = sv[x][3] = 0.f;
+#pragma unroll 1
+    for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+      for (int x = 0; x < QT; ++x) { sv[x][0] = sv[x][2]; sv[x][1] = sv[x][3]; }
+      if ((hf ? b.valid1 : b.valid0) == 0) continue;
+      uint32_t ca[2][KP / 4], nw[2][KW];
+      float2 ab[2];
+      const float* nf[2] = {nullptr, nullptr};
+      uint32_t sl[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int tok = kTile * hf + 8 * r + g;
+#pragma unroll
+        for (int q8 = 0; q8 < KP / 8; ++q8) {
+          const int off = tok * p.k.ab + (t * (KP / 8) + q8) * wk;     // 8 codes: wk bytes
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(st_k + (off & ~3));
+          const int sh_ = (off & 3) * 8;
+          const uint32_t w0 = w[0], w1 = w[1], w2 = w[2];
+          ca[r][2 * q8] = __funnelshift_r(w0, w1, sh_);
+          ca[r][2 * q8 + 1] = __funnelshift_rc(ca[r][2 * q8], __funnelshift_r(w1, w2, sh_), 4 * wk);
+        }
+        ab[r] = kc[tok];
+        sl[r] = __float_as_uint(ab[r].y);          // log: the slope and offset, two halves
+        const uint8_t* nrow = st_kn + tok * p.k.nb;
+        if constexpr (F32N) {
+          nf[r] = reinterpret_cast<const float*>(nrow) + KP * t;
+        } else if constexpr (KW == 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(nrow + 16 * t);
+          nw[r][0] = v.x; nw[r][1] = v.y; nw[r][2] = v.z; nw[r][3] = v.w;
+        } else if constexpr (KW == 2) {
+          const uint2 v = *reinterpret_cast<const uint2*>(nrow + 8 * t);
+          nw[r][0] = v.x; nw[r][1] = v.y;
+        } else {
+          nw[r][0] = *reinterpret_cast<const uint32_t*>(nrow + 4 * t);
+        }
+      }
+      float c1[QT][4], c2[QT][4];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c1[x][i] = c2[x][i] = 0.f;
+      uint4 bq[QT];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if ((ks & 1) == 0) {
+#pragma unroll
+          for (int x = 0; x < QT; ++x) bq[x] = pg_reload(qaddr + (ks / 2 * QT + x) * 512);
+        }
+        uint32_t u[4], y[4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          constexpr bool FAR = KB == 4 && !F32N;   // codes are unpacked four apart
+          const int i0 = FAR ? 8 * (ks >> 2) + (ks & 3) : 2 * ks, i1 = FAR ? i0 + 4 : i0 + 1;
+          u[r] = *reinterpret_cast<const uint32_t*>(tk + ((pg_rotr(ca[r][i0 >> 2], (wk * (i0 & 3) - kTabShift) & 31) & km) | lane_off));
+          u[2 + r] = *reinterpret_cast<const uint32_t*>(tk + ((pg_rotr(ca[r][i1 >> 2], (wk * (i1 & 3) - kTabShift) & 31) & km) | lane_off));
+          uint32_t hb;
+          if constexpr (F32N) {
+            const float2 v = *reinterpret_cast<const float2*>(nf[r] + 2 * ks);
+            hb = ab[r].x == 0.f ? 0u : h2_bits(__floats2half2_rn(v.x * ab[r].y, v.y * ab[r].y));
+          } else if constexpr (LIN) {
+            hb = KB == 8 ? __byte_perm(nw[r][(ks >> 1) % KW], 0u, (ks & 1) ? 0x4342 : 0x4140) : (nw[r][(ks >> 2) % KW] >> (4 * (ks & 3))) & 0x000F000Fu;
+          } else {
+            hb = pg_log_norm<KB>(nw[r][(KB == 8 ? ks >> 1 : ks >> 2) % KW], KB == 8 ? ks & 1 : ks & 3, sl[r]);
+          }
+          y[r] = hmul2(hlow2(hb), u[r]);
+          y[2 + r] = hmul2(hhigh2(hb), u[2 + r]);
+        }
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const uint32_t b0 = ks & 1 ? bq[x].z : bq[x].x, b1 = ks & 1 ? bq[x].w : bq[x].y;
+          pg_mma(c2[x], y, b0, b1);
+          if constexpr (LIN) pg_mma(c1[x], u, b0, b1);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float s2 = c2[x][2 * r] + c2[x][2 * r + 1], s1 = c1[x][2 * r] + c1[x][2 * r + 1];
+          sv[x][2 + r] = qsc[x] * (LIN ? __fmaf_rn(ab[r].x, s1, ab[r].y * s2) : ab[r].x * s2);
+        }
+    }
+  };
+
+  // Rows of the values' fragments are positions, steps run over (token, cos | sin); column 2 a + c has
+  // query a's weights in the rows of component c and zeros in the others, so that a looked-up
+  // (cos, sin) goes in as it is.  w1, w2: the weights of this lane's tokens g, g + 8 of a tile (query
+  // 4 x + t) as two halves; they are handed to the lanes that need them by shuffles.
+  const uint32_t put0 = g & 1 ? 0x1044u : 0x4410u, put1 = g & 1 ? 0x3244u : 0x4432u;
+  auto values_mma = [&](const uint32_t (&w1)[QT][2], const uint32_t (&w2)[QT][2], auto nc_) {
+    constexpr int NC = decltype(nc_)::value;
+    constexpr bool F32N = NC == 4, LIN = NC == 0 || NC == 2;
+    constexpr int VB = NC <= 1 ? 4 : 8;
+    constexpr bool N16 = VB == 4 && VP == 4 && !F32N;    // a token's norms are 16 bits: two tokens in a word
+    constexpr int VW = F32N ? 1 : (VP * VB + 31) / 32;
+    const int wv = p.v.w;
+    const int vbit = VP * g * wv, vsh = vbit & 31;       // a run starts at a byte (VP = 8) or half a byte
+    const uint8_t* const va = st_v + (vbit >> 5) * 4;
+#pragma unroll 1
+    for (int hf = 0; hf < 2; ++hf) {
+      if ((hf ? b.valid1 : b.valid0) == 0) continue;
+      uint32_t p1[QT][2], p2[QT][2];               // tokens t, t + 8 | t + 4, t + 12 of query g / 2
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int src = 4 * (t + 4 * i) + (g >> 1);
+          const uint32_t v2 = hf ? w2[x][1] : w2[x][0], v1 = hf ? w1[x][1] : w1[x][0];
+          p2[x][i] = __shfl_sync(0xffffffffu, v2, src);
+          if constexpr (LIN) p1[x][i] = __shfl_sync(0xffffffffu, v1, src);
+        }
+#pragma unroll
+      for (int s8 = 0; s8 < 2; ++s8) {
+        uint32_t ca[2][VP / 4], nw[2][VW], sl[2];
+        const float* nf[2] = {nullptr, nullptr};
+        float fs[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int tok = kTile * hf + 8 * s8 + 4 * i + t;
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(va + tok * p.v.ab);
+          const uint32_t q0 = w[0], q1 = w[1];
+          ca[i][0] = __funnelshift_r(q0, q1, vsh);
+          if constexpr (VP == 8) ca[i][1] = __funnelshift_rc(ca[i][0], __funnelshift_r(q1, w[2], vsh), 4 * wv);
+          const uint8_t* nrow = st_vn + tok * p.v.nb;
+          sl[i] = vd[tok];
+          if constexpr (F32N) {
+            nf[i] = reinterpret_cast<const float*>(nrow) + VP * g;
+            fs[i] = __uint_as_float(sl[i]);
+          } else if constexpr (VW == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(nrow + 8 * g);
+            nw[i][0] = v.x; nw[i][1] = v.y;
+          } else if constexpr (N16) {
+            nw[i][0] = *reinterpret_cast<const uint16_t*>(nrow + 2 * g);
+          } else {
+            nw[i][0] = *reinterpret_cast<const uint32_t*>(nrow + 4 * g);
+          }
+        }
+        if constexpr (N16) {                       // (token 0, token 1) of a position in one pair of halves
+          nw[0][0] |= nw[1][0] << 16;
+          const uint32_t a = sl[0], c = sl[1];
+          sl[0] = __byte_perm(a, c, 0x5410);       // slopes
+          sl[1] = __byte_perm(a, c, 0x7632);       // offsets
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          constexpr bool FAR = VB == 4 && !F32N && !N16;
+          const int j0 = FAR ? m : 2 * m, j1 = FAR ? m + 4 : 2 * m + 1;
+          uint32_t u[4], y[4], hb[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            u[2 * i] = *reinterpret_cast<const uint32_t*>(tv + ((pg_rotr(ca[i][j0 >> 2], (wv * (j0 & 3) - kTabShift) & 31) & vm) | lane_off));
+            u[2 * i + 1] = *reinterpret_cast<const uint32_t*>(tv + ((pg_rotr(ca[i][j1 >> 2], (wv * (j1 & 3) - kTabShift) & 31) & vm) | lane_off));
+            if constexpr (F32N) {
+              const float2 v = *reinterpret_cast<const float2*>(nf[i] + 2 * m);
+              hb[i] = fs[i] == 0.f ? 0u : h2_bits(__floats2half2_rn(v.x * fs[i], v.y * fs[i]));
+            } else if constexpr (N16) {
+              const int j = i ? j1 : j0;
+              if constexpr (LIN) hb[i] = (nw[0][0] >> (4 * j)) & 0x000F000Fu;
+              else hb[i] = pg_log_norm4(nw[0][0], j, sl[0], sl[1]);
+            } else if constexpr (LIN) {
+              hb[i] = VB == 8 ? __byte_perm(nw[i][(m >> 1) % VW], 0u, (m & 1) ? 0x4342 : 0x4140) : (nw[i][0] >> (4 * m)) & 0x000F000Fu;
+            } else {
+              hb[i] = pg_log_norm<VB>(nw[i][(VB == 8 ? m >> 1 : 0) % VW], VB == 8 ? m & 1 : m, sl[i]);
+            }
+          }
+          if constexpr (N16) {                     // hb[i]: position j_i of tokens 0 | 1
+            y[0] = hmul2(hlow2(hb[0]), u[0]);
+            y[1] = hmul2(hlow2(hb[1]), u[1]);
+            y[2] = hmul2(hhigh2(hb[0]), u[2]);
+            y[3] = hmul2(hhigh2(hb[1]), u[3]);
+          } else {                                 // hb[i]: positions j0 | j1 of token i
+            y[0] = hmul2(hlow2(hb[0]), u[0]);
+            y[1] = hmul2(hhigh2(hb[0]), u[1]);
+            y[2] = hmul2(hlow2(hb[1]), u[2]);
+            y[3] = hmul2(hhigh2(hb[1]), u[3]);
+          }
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            const uint32_t put = s8 ? put1 : put0;
+            pg_mma(am[x][m], y, __byte_perm(p2[x][0], 0u, put), __byte_perm(p2[x][1], 0u, put));
+            if constexpr (LIN) pg_mma(am[x][m], u, __byte_perm(p1[x][0], 0u, put), __byte_perm(p1[x][1], 0u, put));
+          }
+        }
+      }
+    }
+  };
+
+  // fp32 norms: no header; the largest norm of each token of the batch sets its power of two.
+  // out[token] = 2^-e with r^ 2^-e in [0.5, 1) for the largest; returns 2^e of token `lane`.
+  auto fp32_scale = [&](const uint8_t* norms, int row_bytes) {
+    float mine = 0.f;
+    for (int i = 0; i < kBatch / 4; ++i) {
+      const float* nr = reinterpret_cast<const float*>(norms + (4 * i + (lane >> 3)) * row_bytes) + VP * (lane & 7);
+      float mx = 0.f;
+#pragma unroll
+      for (int k = 0; k < VP; k += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(nr + k);
+        mx = fmaxf(fmaxf(fmaxf(mx, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      mx = __shfl_sync(0xffffffffu, mx, 8 * (lane & 3));
+      if ((lane >> 2) == i) mine = mx;
+    }
+    return pg_exp2i(pg_exp_of(mine) + 1);
+  };
+  const bool v_far = p.v.nc <= 1 && VP == 8;       // the order of the values' row tiles
+
   while (more) {
     b = nx;
     if (b.begins) {                                // a new (sequence, head)
@@ -651,19 +946,55 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 #pragma unroll
         for (int k = 0; k < E; ++k) y[k] = 0.f;
         if (a < p.group) pg_load_query<D>(p, bf, b.seq, b.head, a, lane, y);
+        if constexpr (EXACT) {
 #pragma unroll
-        for (int k = 0; k < E; k += 2) {           // pair (E lane + k) / 2
-          const int i = pair_slot<D>((E * lane + k) / 2);
-          *reinterpret_cast<float2*>(pw + C::W_Q + (a * 4 + i / KP) * C::QRUN + (i % KP) * 8) = make_float2(y[k], y[k + 1]);
+          for (int k = 0; k < E; k += 2) {         // pair (E lane + k) / 2
+            const int i = pair_slot<D>((E * lane + k) / 2);
+            *reinterpret_cast<float2*>(pw + C::W_Q + (a * 4 + i / KP) * C::QRUN + (i % KP) * 8) = make_float2(y[k], y[k + 1]);
+          }
+        } else {
+          // over the power of two that brings the largest element to [2^13, 2^14); then the fp16
+          // number next to each element and what is left, where the step that takes them loads them
+          float mx = 0.f;
+#pragma unroll
+          for (int k = 0; k < E; ++k) mx = fmaxf(mx, fabsf(y[k]));
+#pragma unroll
+          for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const int ex = min(max(pg_exp_of(mx) - 13, -126), 126);
+          const float sc = pg_exp2i(-ex);
+          if (lane == 0) reinterpret_cast<float*>(pw + C::W_QS)[a] = pg_exp2i(ex);
+#pragma unroll
+          for (int k = 0; k < E; k += 2) {
+            const int i = pair_slot<D>((E * lane + k) / 2), r = i % KP;
+            const int at = p.k.nc <= 1 ? (r & ~7) + 2 * (r & 3) + ((r >> 2) & 1) : r;     // 4-bit norms: four apart
+            uint32_t* const w = reinterpret_cast<uint32_t*>(pw + C::W_Q) + (((at >> 2) * QT + (a >> 2)) * 32 + 8 * (a & 3) + i / KP) * 4 + (at & 3);
+            const float q0 = y[k] * sc, q1 = y[k + 1] * sc;
+            const __half2 hi = __floats2half2_rn(q0, q1);
+            const float2 back = __half22float2(hi);
+            w[0] = h2_bits(hi);
+            w[16] = h2_bits(__floats2half2_rn(q0 - back.x, q1 - back.y));
+          }
         }
       }
       __syncwarp();
 #pragma unroll
       for (int x = 0; x < QT; ++x) { m_[x] = -INFINITY; l_[x] = 0.f; }
+      if constexpr (EXACT) {
 #pragma unroll
-      for (int a = 0; a < NQ; ++a)
+        for (int a = 0; a < NQ; ++a)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[a][j] = make_float2(0.f, 0.f);
+          for (int j = 0; j < 4; ++j) acc[a][j] = make_float2(0.f, 0.f);
+      } else {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          ae[x] = -126;
+          qsc[x] = reinterpret_cast<const float*>(pw + C::W_QS)[4 * x + t];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) am[x][m][i] = 0.f;
+        }
+      }
     }
     more = cursor_next(p, cur, lane, nx);
     if (more) nx.begins = b.ends;
@@ -672,66 +1003,175 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     float sv[QT][4];
     const bool alive = (lane < kTile ? lane < b.valid0 : lane - kTile < b.valid1);   // token `lane` counts
     if (any) {
-      kc[lane] = pg_norm_consts(st_kh, p.k.nc, lane, alive);
-      __syncwarp();
-      switch (p.k.nc) {
-        case 0: scores(sv, IC<0>{}); break;
-        case 1: scores(sv, IC<1>{}); break;
-        case 2: scores(sv, IC<2>{}); break;
-        case 3: scores(sv, IC<3>{}); break;
-        default: scores(sv, IC<4>{}); break;
+      if constexpr (EXACT) {
+        kc[lane] = pg_norm_consts(st_kh, p.k.nc, lane, alive);
+        __syncwarp();
+        switch (p.k.nc) {
+          case 0: scores(sv, IC<0>{}); break;
+          case 1: scores(sv, IC<1>{}); break;
+          case 2: scores(sv, IC<2>{}); break;
+          case 3: scores(sv, IC<3>{}); break;
+          default: scores(sv, IC<4>{}); break;
+        }
+      } else {
+        // K's constants: linear (r_min, Delta), log (r_max, slope | offset), fp32 (2^e, 2^-e), over the
+        // units of the products; zeros for a token that does not count
+        float2 k2 = make_float2(0.f, 0.f);
+        if (p.k.nc == 4) {
+          const float f = fp32_scale(st_kn, p.k.nb);
+          if (alive) k2 = make_float2(f * (1.f / kUnit), 1.f / f);
+        } else if (alive) {
+          const float2 h = reinterpret_cast<const float2*>(st_kh)[lane];
+          if (p.k.nc & 1) {
+            float f;
+            k2.y = __uint_as_float(pg_log_consts(h, p.k.nc, f));
+            k2.x = f * (1.f / kUnit);
+          } else {
+            k2.x = h.x * (1.f / kUnit);
+            k2.y = (h.y > h.x ? (h.y - h.x) * (p.k.nc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * (16777216.f / kUnit);
+          }
+        }
+        kc[lane] = k2;
+        __syncwarp();
+        switch (p.k.nc) {
+          case 0: scores_mma(sv, IC<0>{}); break;
+          case 1: scores_mma(sv, IC<1>{}); break;
+          case 2: scores_mma(sv, IC<2>{}); break;
+          case 3: scores_mma(sv, IC<3>{}); break;
+          default: scores_mma(sv, IC<4>{}); break;
+        }
       }
       __syncwarp();                                // every lane is done with the K rows
     }
     if (more) issue(false, nx);
-    if (any) {
-      bool moved = false;
-      float fix[QT];
+    if constexpr (EXACT) {
+      if (any) {
+        bool moved = false;
+        float fix[QT];
 #pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        float mx = -INFINITY;
+        for (int x = 0; x < QT; ++x) {
+          float mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int o = 8 * (i & 1) + g;
-          if (o >= (i >> 1 ? b.valid1 : b.valid0)) sv[x][i] = -INFINITY;
-          mx = fmaxf(mx, sv[x][i]);
+          for (int i = 0; i < 4; ++i) {
+            const int o = 8 * (i & 1) + g;
+            if (o >= (i >> 1 ? b.valid1 : b.valid0)) sv[x][i] = -INFINITY;
+            mx = fmaxf(mx, sv[x][i]);
+          }
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float mn = fmaxf(m_[x], mx), ref = mn == -INFINITY ? 0.f : mn;
+          fix[x] = ex2_approx(m_[x] - ref);
+          moved |= mn > m_[x];
+          m_[x] = mn;
+          l_[x] *= fix[x];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float pr = ex2_approx(sv[x][i] - ref);
+            l_[x] += pr;
+            wt[(16 * (i >> 1) + 8 * (i & 1) + g) * NQ + 4 * x + t] = pr;
+          }
         }
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float mn = fmaxf(m_[x], mx), ref = mn == -INFINITY ? 0.f : mn;
-        fix[x] = ex2_approx(m_[x] - ref);
-        moved |= mn > m_[x];
-        m_[x] = mn;
-        l_[x] *= fix[x];
+          for (int a = 0; a < NQ; ++a) {
+            const float f = __shfl_sync(0xffffffffu, fix[a >> 2], a & 3);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float pr = ex2_approx(sv[x][i] - ref);
-          l_[x] += pr;
-          wt[(16 * (i >> 1) + 8 * (i & 1) + g) * NQ + 4 * x + t] = pr;
+            for (int j = 0; j < 4; ++j) acc[a][j] = mul2(acc[a][j], make_float2(f, f));
+          }
         }
       }
-      if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-        for (int a = 0; a < NQ; ++a) {
-          const float f = __shfl_sync(0xffffffffu, fix[a >> 2], a & 3);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[a][j] = mul2(acc[a][j], make_float2(f, f));
+      landed(b, bar_v, phase_v);
+      if (any) {
+        vc[lane] = pg_norm_consts(st_vh, p.v.nc, lane, alive);
+        __syncwarp();
+        const int tokens = b.valid1 > 0 ? kBatch : kTile;
+        switch (p.v.nc) {
+          case 0: values(tokens, IC<0>{}); break;
+          case 1: values(tokens, IC<1>{}); break;
+          case 2: values(tokens, IC<2>{}); break;
+          case 3: values(tokens, IC<3>{}); break;
+          default: values(tokens, IC<4>{}); break;
         }
+        __syncwarp();                              // every lane is done with the V rows
       }
-    }
-    landed(b, bar_v, phase_v);
-    if (any) {
-      vc[lane] = pg_norm_consts(st_vh, p.v.nc, lane, alive);
-      __syncwarp();
-      const int tokens = b.valid1 > 0 ? kBatch : kTile;
-      switch (p.v.nc) {
-        case 0: values(tokens, IC<0>{}); break;
-        case 1: values(tokens, IC<1>{}); break;
-        case 2: values(tokens, IC<2>{}); break;
-        case 3: values(tokens, IC<3>{}); break;
-        default: values(tokens, IC<4>{}); break;
+    } else {
+      landed(b, bar_v, phase_v);
+      if (any) {
+        // V's factors: linear (r_min, 2^24 Delta), log (., r_max) and the slope, fp32 (., 2^e) and 2^-e
+        float2 f2 = make_float2(0.f, 0.f);
+        uint32_t d2 = 0u;
+        if (p.v.nc == 4) {
+          const float f = fp32_scale(st_vn, p.v.nb);
+          if (alive) { f2.y = f; d2 = __float_as_uint(1.f / f); }
+        } else if (alive) {
+          const float2 h = reinterpret_cast<const float2*>(st_vh)[lane];
+          if (p.v.nc & 1) {
+            d2 = pg_log_consts(h, p.v.nc, f2.y);
+          } else {
+            f2.x = h.x;
+            f2.y = (h.y > h.x ? (h.y - h.x) * (p.v.nc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * 16777216.f;
+          }
+        }
+        vc[lane] = f2;
+        vd[lane] = d2;
+        __syncwarp();
+        // softmax (base 2) against the whole number above the largest score so far; the weights
+        // times V's factors over a power of two that keeps the largest so far below 2^14
+        uint32_t w1[QT][2], w2[QT][2];
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int o = 8 * (i & 1) + g;
+            if (o >= (i >> 1 ? b.valid1 : b.valid0)) sv[x][i] = -INFINITY;
+            mx = fmaxf(mx, sv[x][i]);
+          }
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float mn = fmaxf(m_[x], ceilf(mx)), ref = mn == -INFINITY ? 0.f : mn;
+          float wa[4], wb[4], wm = 0.f;
+          const float fix = ex2_approx(m_[x] - ref);         // a whole power of two, or 0
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float pr = ex2_approx(sv[x][i] - ref);
+            const float2 f = vc[16 * (i >> 1) + 8 * (i & 1) + g];
+            sum += pr;
+            wa[i] = pr * f.x;
+            wb[i] = pr * f.y;
+            wm = fmaxf(wm, fmaxf(wa[i], wb[i]));
+          }
+          l_[x] = __fmaf_rn(l_[x], fix, sum);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+          const int ex = max(ae[x], min(pg_exp_of(wm) - 13, 126));
+          const bool moved = mn > m_[x] || ex > ae[x];
+          if (__any_sync(0xffffffffu, moved)) {
+            const float f = fix * (ex > ae[x] + 252 ? 0.f : pg_exp2i((ae[x] - ex) / 2) * pg_exp2i((ae[x] - ex) - (ae[x] - ex) / 2));
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) am[x][m][i] *= f;
+          }
+          m_[x] = mn;
+          ae[x] = ex;
+          const float sc = pg_exp2i(-ex);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            w1[x][i] = h2_bits(__floats2half2_rn(wa[2 * i] * sc, wa[2 * i + 1] * sc));
+            w2[x][i] = h2_bits(__floats2half2_rn(wb[2 * i] * sc, wb[2 * i + 1] * sc));
+          }
+        }
+        switch (p.v.nc) {
+          case 0: values_mma(w1, w2, IC<0>{}); break;
+          case 1: values_mma(w1, w2, IC<1>{}); break;
+          case 2: values_mma(w1, w2, IC<2>{}); break;
+          case 3: values_mma(w1, w2, IC<3>{}); break;
+          default: values_mma(w1, w2, IC<4>{}); break;
+        }
+        __syncwarp();                              // every lane is done with the V rows
       }
-      __syncwarp();                                // every lane is done with the V rows
     }
     if (more) issue(true, nx);
     if (b.ends) {
@@ -743,6 +1183,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
       for (int x = 0; x < QT; ++x)
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l_[x] += __shfl_xor_sync(0xffffffffu, l_[x], o);
+      if constexpr (EXACT) {
 #pragma unroll
       for (int a = 0; a < NQ; ++a)
 #pragma unroll
@@ -754,6 +1195,20 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
           }
           if (vt == 0) *reinterpret_cast<float2*>(rec + a * pg_rec_floats(D) + 2 + 2 * slot_pair<D>(4 * vl + j)) = acc[a][j];
         }
+      } else {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const float f = pg_exp2i(ae[x]) * (1.f / kUnit);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int j = v_far ? m + 4 * i : 2 * m + i;
+              *reinterpret_cast<float2*>(rec + (4 * x + t) * pg_rec_floats(D) + 2 + 2 * slot_pair<D>(VP * g + j)) =
+                  make_float2(am[x][m][2 * i] * f, am[x][m][2 * i + 1] * f);
+            }
+        }
+      }
       if (g == 0) {
 #pragma unroll
         for (int x = 0; x < QT; ++x)
@@ -876,10 +1331,10 @@ static cudaError_t launch_join(const AttPagesParams& p, bool bf, cudaStream_t st
   return cudaLaunchKernelEx(&cfg, attend_pages_join<D>, p, (int)bf);
 }
 
-template <int D, int QT>
-static cudaError_t launch_f32_t(const AttPagesParams& p, bool bf, cudaStream_t st) {
-  using C = PgF<D, QT>;
-  auto kp = attend_pages_f32<D, QT>;
+template <int D, int QT, bool EXACT>
+static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
+  using C = Pg<D, QT, EXACT>;
+  auto kp = attend_pages_kernel<D, QT, EXACT>;
   static std::atomic<int> ready[64];
   cudaError_t e = set_smem_once(kp, ready);
   if (e != cudaSuccess) return e;
@@ -887,19 +1342,23 @@ static cudaError_t launch_f32_t(const AttPagesParams& p, bool bf, cudaStream_t s
   const int tabs = tab_v + ((1 << p.v.w) << kTabShift);
   const int warp_bytes = (C::W_STG + pg_stage_bytes(p.k) + pg_stage_bytes(p.v) + 127) / 128 * 128;
   const int nw = std::min(kMaxWarps, (227 * 1024 - (int)sizeof(PgShared) - 256 - tabs) / warp_bytes);
-  kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, (int)bf, tab_v, warp_bytes);
+  kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, tab_v, warp_bytes);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_join<D>(p, bf, st);
+  return launch_join<D>(p, !EXACT, st);
 }
 
 // CTAs of the main kernel: one on every SM.
 int attend_pages_ctas(int, int, int, int sms) { return std::min(sms, kAttPgMaxCtas); }
 
 cudaError_t launch_attend_pages(int d, int dtype, const AttPagesParams& p, cudaStream_t st) {
-  const bool bf = dtype == TAC_BF16;
-  if (d == 128) return p.group <= 4 ? launch_f32_t<128, 1>(p, bf, st) : launch_f32_t<128, 2>(p, bf, st);
-  return p.group <= 4 ? launch_f32_t<64, 1>(p, bf, st) : launch_f32_t<64, 2>(p, bf, st);
+  const bool wide = p.group > 4;
+  if (dtype == TAC_BF16) {
+    if (d == 128) return wide ? launch_pages_t<128, 2, false>(p, st) : launch_pages_t<128, 1, false>(p, st);
+    return wide ? launch_pages_t<64, 2, false>(p, st) : launch_pages_t<64, 1, false>(p, st);
+  }
+  if (d == 128) return wide ? launch_pages_t<128, 2, true>(p, st) : launch_pages_t<128, 1, true>(p, st);
+  return wide ? launch_pages_t<64, 2, true>(p, st) : launch_pages_t<64, 1, true>(p, st);
 }
 
 }  // namespace tac

@@ -54,6 +54,11 @@ __device__ __forceinline__ void pg_bar_init(uint32_t bar) {
 __device__ __forceinline__ void pg_bar_expect(uint32_t bar, int bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ bool pg_elect() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ void pg_copy(uint32_t dst, const void* src, int bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(bar)
@@ -190,91 +195,87 @@ __device__ __forceinline__ int pg_tiles(const AttPagesParams& p, int i) {
   return min(max(p.counts[i], 0), p.budget) * (p.pg.page / kTile);
 }
 
-// Walks a warp's tiles in order.
+// Walks a warp's tiles in order, two (a batch) at a time.  The places of up to 32 batches are
+// worked out at once, one a lane, and handed out by shuffles.
 struct Cursor {
-  int64_t left;          // tiles still to come
-  int item, head;        // the (sequence, head) of the next tile
-  int seq;
-  int i, nt;             // next tile within it, its tiles
-  int len;               // the sequence's tokens
-  int ent, sub;          // page entry and tile within the page of tile i
-  int base;              // first page entry held in the lanes' registers (a multiple of 32)
-  int phys, logical;     // lane l: page and table column of entry base + l (page -1: none)
+  int64_t left;          // tiles still to come, behind the window
+  int item, head, seq;   // the (sequence, head) of the window
+  int i, nt;             // the tile behind the window, the (sequence, head)'s tiles
+  int j, n;              // next batch of the window, its batches
+  bool first, done;      // the window starts with tile 0; ends this warp's part of the (sequence, head)
+  uint32_t t0, t1;       // lane l: first record slots / 16 of batch l's two tiles
+  uint32_t valid;        // and how many tokens of each count (16 bits each; 0: nothing is copied)
 };
-
-__device__ __forceinline__ void cursor_pages(const AttPagesParams& p, Cursor& c, int lane) {
-  c.base = c.ent & ~31;
-  const int e = c.base + lane;
-  int col = -1;
-  if (p.selected) {
-    const int have = c.nt / (p.pg.page / kTile);
-    if (e < have) col = p.selected[((int64_t)c.seq * p.pg.heads + c.head) * p.budget + e];
-  } else if (e < p.pg.width) {
-    col = e;
-  }
-  int ph = -1;
-  if (col >= 0 && col < p.pg.width && (int64_t)col * p.pg.page < c.len) ph = p.pg.table[(int64_t)c.seq * p.pg.table_stride + col];
-  c.phys = ph >= 0 && ph < p.pg.pages ? ph : -1;
-  c.logical = col;
-}
-
-// The cursor at tile i of (item, head).
-__device__ __forceinline__ void cursor_open(const AttPagesParams& p, Cursor& c, int lane) {
-  c.seq = p.selected ? c.item / p.pg.heads : c.item;
-  if (p.selected) c.head = c.item % p.pg.heads;
-  c.len = pg_len(p, c.seq);
-  const int per = p.pg.page / kTile;
-  c.ent = c.i / per;
-  c.sub = c.i - c.ent * per;
-  cursor_pages(p, c, lane);
-}
 
 // A batch: two tiles (the second may be missing) of one (sequence, head).
 struct Batch {
-  int64_t slot0, slot1;  // first record slots
+  uint32_t t0, t1;       // first record slots / 16
   int valid0, valid1;    // tokens of each tile that count (0: nothing is copied)
   int seq, head;
   bool begins, first;    // the warp's first batch of this (sequence, head); which starts with tile 0
   bool ends, last;       // the warp's last batch of it; which holds its last tile
 };
 
-__device__ __forceinline__ void cursor_tile(const AttPagesParams& p, Cursor& c, int lane, int64_t& slot, int& valid) {
-  if (c.ent >= c.base + 32) cursor_pages(p, c, lane);
-  const int ph = __shfl_sync(0xffffffffu, c.phys, c.ent - c.base), col = __shfl_sync(0xffffffffu, c.logical, c.ent - c.base);
-  const int64_t pos = (int64_t)col * p.pg.page + c.sub * kTile;
-  valid = ph < 0 ? 0 : (int)min(max(c.len - pos, (int64_t)0), (int64_t)kTile);
-  slot = ((int64_t)ph * p.pg.heads + c.head) * p.pg.page + c.sub * kTile;
-  ++c.i;
-  if (++c.sub * kTile == p.pg.page) { c.sub = 0; ++c.ent; }
+// Where tile i of the cursor's (sequence, head) is, and how many of its tokens count.
+__device__ __forceinline__ void cursor_tile(const AttPagesParams& p, const Cursor& c, int len, int i, uint32_t& at, uint32_t& valid) {
+  const int per = p.pg.page / kTile, ent = i / per, sub = i - ent * per;
+  int col = ent;
+  if (p.selected) col = p.selected[((int64_t)c.seq * p.pg.heads + c.head) * p.budget + ent];
+  at = valid = 0;
+  if (col < 0 || col >= p.pg.width) return;
+  const int pos = col * p.pg.page + sub * kTile;
+  if (pos >= len) return;
+  const int ph = p.pg.table[(int64_t)c.seq * p.pg.table_stride + col];
+  if (ph < 0 || ph >= p.pg.pages) return;
+  at = (uint32_t)(((int64_t)ph * p.pg.heads + c.head) * per + sub);
+  valid = (uint32_t)min(len - pos, kTile);
+}
+
+__device__ __forceinline__ void cursor_fill(const AttPagesParams& p, Cursor& c, int lane) {
+  while (c.i >= c.nt) {                            // to the next (sequence, head) that has tiles
+    if (p.selected || ++c.head == p.pg.heads) {
+      c.head = 0;
+      c.nt = pg_tiles(p, ++c.item);
+    }
+    c.i = 0;
+  }
+  c.seq = c.item;
+  if (p.selected) {
+    c.seq = c.item / p.pg.heads;
+    c.head = c.item - c.seq * p.pg.heads;
+  }
+  const int len = pg_len(p, c.seq);
+  const int m = (int)min(c.left, (int64_t)(c.nt - c.i)), take = min(m, 64);
+  uint32_t v0 = 0, v1 = 0;
+  c.t0 = c.t1 = 0;
+  if (2 * lane < take) cursor_tile(p, c, len, c.i + 2 * lane, c.t0, v0);
+  if (2 * lane + 1 < take) cursor_tile(p, c, len, c.i + 2 * lane + 1, c.t1, v1);
+  c.valid = v0 | v1 << 16;
+  c.first = c.i == 0;
+  c.j = 0;
+  c.n = (take + 1) / 2;
+  c.i += take;
+  c.left -= take;
+  c.done = take == m;
 }
 
 // The next batch; false when the warp's tiles are done.
 __device__ __forceinline__ bool cursor_next(const AttPagesParams& p, Cursor& c, int lane, Batch& b) {
-  if (c.left <= 0) return false;
-  bool opened = false;
-  while (c.i >= c.nt) {                            // to the next (sequence, head) that has tiles
-    if (p.selected || ++c.head == p.pg.heads) {
-      c.head = 0;
-      ++c.item;
-      c.nt = pg_tiles(p, c.item);
-    }
-    c.i = 0;
-    opened = true;
+  if (c.j == c.n) {
+    if (c.left <= 0) return false;
+    cursor_fill(p, c, lane);
   }
-  if (opened) cursor_open(p, c, lane);
+  b.t0 = __shfl_sync(0xffffffffu, c.t0, c.j);
+  b.t1 = __shfl_sync(0xffffffffu, c.t1, c.j);
+  const uint32_t v = __shfl_sync(0xffffffffu, c.valid, c.j);
+  b.valid0 = (int)(v & 0xFFFFu);
+  b.valid1 = (int)(v >> 16);
   b.seq = c.seq;
   b.head = c.head;
-  b.first = c.i == 0;
-  cursor_tile(p, c, lane, b.slot0, b.valid0);
-  --c.left;
-  b.slot1 = 0;
-  b.valid1 = 0;
-  if (c.i < c.nt && c.left > 0) {
-    cursor_tile(p, c, lane, b.slot1, b.valid1);
-    --c.left;
-  }
-  b.last = c.i == c.nt;
-  b.ends = b.last || c.left == 0;
+  b.first = c.first && c.j == 0;
+  ++c.j;
+  b.ends = c.done && c.j == c.n;
+  b.last = b.ends && c.i == c.nt;
   return true;
 }
 
@@ -403,6 +404,7 @@ __device__ __forceinline__ int64_t pg_plan(const AttPagesParams& p, PgShared& sh
     }
   }
   c.left = 0;
+  c.j = c.n = 0;
   if ((int64_t)blockIdx.x >= nc) return 0;
   const int64_t W = nc * nw, me = (int64_t)blockIdx.x * nw + warp;
   int64_t t0 = total * me / W;
@@ -423,7 +425,6 @@ __device__ __forceinline__ int64_t pg_plan(const AttPagesParams& p, PgShared& sh
   c.nt = n;
   c.head = (int)(t0 / n);
   c.i = (int)(t0 - (int64_t)c.head * n);
-  cursor_open(p, c, lane);
   return total;
 }
 
@@ -455,6 +456,60 @@ __device__ __forceinline__ float pg_norm(const uint32_t* w, int j, float2 ab) {
     return NC & 1 ? ex2_ftz(r) : r;
   }
 }
+
+// The codes of a lane's run of N (4, 8 or 16): W bits each, known at compile time, or `w` where W is 0.
+// words(): from the run's first byte on; offset(i): the byte offset of code i's table entry, to be
+// masked.  Known widths take the words as they are and codes by one funnel shift; otherwise every
+// four codes are brought into a word of their own and taken by a rotation.
+template <int W, int N>
+struct Run {
+  static constexpr int NW = W ? (N * W + 31) / 32 : (N + 3) / 4;
+  uint32_t x[NW];
+  // base: the word the run starts in (4-byte aligned), sh: its first bit there
+  __device__ __forceinline__ void load(const uint8_t* base, int sh, int w) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(base);
+    if constexpr (W != 0) {
+      if constexpr ((N * W) % 32 == 0) {           // whole words
+        if constexpr (NW == 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(p);
+          x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else if constexpr (NW == 2) {
+          const uint2 v = *reinterpret_cast<const uint2*>(p);
+          x[0] = v.x; x[1] = v.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < NW; ++i) x[i] = p[i];
+        }
+      } else {                                     // W = 6: the run ends inside its last word
+        uint32_t a = p[0];
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+          const uint32_t b = i + 1 < NW || (N * W) % 32 > 16 ? p[i + 1] : 0u;
+          x[i] = __funnelshift_r(a, b, sh);
+          a = b;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < NW; q += 2) {            // eight codes: w bytes
+        const int bit = sh + 8 * w * (q / 2);
+        const uint32_t* r = p + (bit >> 5);
+        const uint32_t a = r[0], b = r[1];
+        x[q] = __funnelshift_r(a, b, bit & 31);
+        if (q + 1 < NW) x[q + 1] = __funnelshift_rc(x[q], __funnelshift_r(b, r[2], bit & 31), 4 * w);
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t offset(int i, int w) const {
+    if constexpr (W != 0) {
+      const int bit = i * W, at = bit >> 5, sh = (bit & 31) - kTabShift;
+      if (sh >= 0) return at + 1 < NW ? __funnelshift_r(x[at], x[at + 1], sh) : x[at] >> sh;
+      return x[at] << -sh;
+    } else {
+      return pg_rotr(x[i >> 2], (w * (i & 3) - kTabShift) & 31);
+    }
+  }
+};
 
 // 2^(log2 r^ - log2 r_max) of two norms as halves.  4-bit codes j and j + 4 of a word become the
 // halves 16 + c (the code in the mantissa's upper bits), one fma with slope and offset from
@@ -526,24 +581,32 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   if (total == 0) return;                          // no tile for this CTA
   if (lane == 0) sh.empty[warp] = cur.left <= 0;
 
-  // ---- staging: lane x copies plane x % 3 (angle | norm | header) of tile (x / 3) % 2, of K
-  // (x < 6) or V ----
-  const bool c_v = lane >= 6;
-  const int c_plane = lane % 3, c_half = (lane / 3) & 1;
-  const Book& cb = c_v ? p.v : p.k;
-  const int c_row = lane >= 12 ? 0 : c_plane == 0 ? cb.ab : c_plane == 1 ? cb.nb : cb.hb;
-  const uint8_t* const c_src = c_plane == 0 ? cb.codes : c_plane == 1 ? cb.norms : cb.hdr;
-  const uint32_t c_dst = pg_smem(c_plane == 0 ? (c_v ? st_v : st_k) : c_plane == 1 ? (c_v ? st_vn : st_kn) : (c_v ? st_vh : st_kh)) +
-                         c_half * kTile * c_row;
-  const int tile_k = kTile * (p.k.ab + p.k.nb + p.k.hb), tile_v = kTile * (p.v.ab + p.v.nb + p.v.hb);
+  // ---- staging: one lane (elected, so that the compiler knows it is one) copies the planes (angle | norm | header) of a batch's tiles, both at
+  // once where they lie side by side ----
   uint32_t phase_k = 0, phase_v = 0;
   bool dead = false;                               // a wait ran out
-  auto issue = [&](bool v, const Batch& b) {
+  auto copy_rows = [&](const Book& bk, uint32_t stage, uint32_t bar, uint32_t tile, int half, int rows) {
+    const int64_t slot = (int64_t)tile * kTile;
+    const int row = half * kTile;
+    pg_copy(stage + row * bk.ab, bk.codes + slot * bk.ab, rows * bk.ab, bar);
+    pg_copy(stage + kBatch * bk.ab + row * bk.nb, bk.norms + slot * bk.nb, rows * bk.nb, bar);
+    if (bk.hb) pg_copy(stage + kBatch * (bk.ab + bk.nb) + row * 8, bk.hdr + slot * 8, rows * 8, bar);
+  };
+  const uint32_t stage_k = pg_smem(st_k), stage_v = pg_smem(st_v);
+  auto issue = [&](const Book& bk, uint32_t stage, uint32_t bar, const Batch& b) {
     if (dead || (b.valid0 | b.valid1) == 0) return;
-    if (lane == 0) pg_bar_expect(v ? bar_v : bar_k, ((b.valid0 > 0) + (b.valid1 > 0)) * (v ? tile_v : tile_k));
+    if (pg_elect()) {
+      const int tile = kTile * (bk.ab + bk.nb + bk.hb);
+      if (b.valid0 && b.valid1 && b.t1 == b.t0 + 1) {
+        pg_bar_expect(bar, 2 * tile);
+        copy_rows(bk, stage, bar, b.t0, 0, kBatch);
+      } else {
+        pg_bar_expect(bar, ((b.valid0 > 0) + (b.valid1 > 0)) * tile);
+        if (b.valid0) copy_rows(bk, stage, bar, b.t0, 0, kTile);
+        if (b.valid1) copy_rows(bk, stage, bar, b.t1, 1, kTile);
+      }
+    }
     __syncwarp();
-    if (c_v == v && c_row > 0 && (c_half ? b.valid1 : b.valid0) > 0)
-      pg_copy(c_dst, c_src + (c_half ? b.slot1 : b.slot0) * c_row, kTile * c_row, v ? bar_v : bar_k);
   };
   auto landed = [&](const Batch& b, uint32_t bar, uint32_t& phase) {
     if ((b.valid0 | b.valid1) != 0 && !dead) {
@@ -556,8 +619,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   bool more = cursor_next(p, cur, lane, nx);
   if (more) {
     nx.begins = true;
-    issue(false, nx);
-    issue(true, nx);
+    issue(p.k, stage_k, bar_k, nx);
+    issue(p.v, stage_v, bar_v, nx);
   }
 
   // ---- bin-centre tables, every entry 2^kTabShift bytes of copies (EXACT: 16 of two floats, so
@@ -719,48 +782,41 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   // (2^-9.9), r_max outside; fp32 norms over the record's power of two.
   // Rows of the scores' fragments are tokens, steps run over the positions; column 2 a (2 a + 1) is
   // the fp16 number next to query a's element (what is left of it).
-  auto scores_mma = [&](float (&sv)[QT][4], auto nc_) {
-    constexpr int NC = decltype(nc_)::value;
+  auto scores_mma = [&](float (&sv)[QT][4], auto nc_, auto w_) {
+    constexpr int NC = decltype(nc_)::value, W = decltype(w_)::value;
     constexpr bool F32N = NC == 4, LIN = NC == 0 || NC == 2;
     constexpr int KB = NC <= 1 ? 4 : 8, KW = F32N ? 1 : KP * KB / 32;
-    const int wk = p.k.w;
+    const int wk = W ? W : p.k.w, kab = W ? C::P * W / 8 : p.k.ab, kbit = KP * t * wk;
+    constexpr int knb = F32N ? 4 * C::P : C::P * KB / 8;
     const uint32_t qaddr = pg_smem(pw + C::W_Q) + 16 * lane;
+    const uint8_t* arow = st_k + g * kab + (kbit >> 5) * 4;
+    const uint8_t* nrow = st_kn + g * knb + (F32N ? 4 * KP * t : KP * KB / 8 * t);
+    const float2* cst = kc + g;
 #pragma unroll
     for (int x = 0; x < QT; ++x) sv[x][2] = sv[x][3] = 0.f;
 #pragma unroll 1
-    for (int hf = 0; hf < 2; ++hf) {
+    for (int hf = 0; hf < 2; ++hf, arow += kTile * kab, nrow += kTile * knb, cst += kTile) {
 #pragma unroll
       for (int x = 0; x < QT; ++x) { sv[x][0] = sv[x][2]; sv[x][1] = sv[x][3]; }
       if ((hf ? b.valid1 : b.valid0) == 0) continue;
-      uint32_t ca[2][KP / 4], nw[2][KW];
+      Run<W, KP> run[2];
+      uint32_t nw[2][KW], sl[2];
       float2 ab[2];
-      const float* nf[2] = {nullptr, nullptr};
-      uint32_t sl[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int tok = kTile * hf + 8 * r + g;
-#pragma unroll
-        for (int q8 = 0; q8 < KP / 8; ++q8) {
-          const int off = tok * p.k.ab + (t * (KP / 8) + q8) * wk;     // 8 codes: wk bytes
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(st_k + (off & ~3));
-          const int sh_ = (off & 3) * 8;
-          const uint32_t w0 = w[0], w1 = w[1], w2 = w[2];
-          ca[r][2 * q8] = __funnelshift_r(w0, w1, sh_);
-          ca[r][2 * q8 + 1] = __funnelshift_rc(ca[r][2 * q8], __funnelshift_r(w1, w2, sh_), 4 * wk);
-        }
-        ab[r] = kc[tok];
+        run[r].load(arow + 8 * r * kab, kbit & 31, wk);
+        ab[r] = cst[8 * r];
         sl[r] = __float_as_uint(ab[r].y);          // log: the slope and offset, two halves
-        const uint8_t* nrow = st_kn + tok * p.k.nb;
+        const uint8_t* nr = nrow + 8 * r * knb;
         if constexpr (F32N) {
-          nf[r] = reinterpret_cast<const float*>(nrow) + KP * t;
         } else if constexpr (KW == 4) {
-          const uint4 v = *reinterpret_cast<const uint4*>(nrow + 16 * t);
+          const uint4 v = *reinterpret_cast<const uint4*>(nr);
           nw[r][0] = v.x; nw[r][1] = v.y; nw[r][2] = v.z; nw[r][3] = v.w;
         } else if constexpr (KW == 2) {
-          const uint2 v = *reinterpret_cast<const uint2*>(nrow + 8 * t);
+          const uint2 v = *reinterpret_cast<const uint2*>(nr);
           nw[r][0] = v.x; nw[r][1] = v.y;
         } else {
-          nw[r][0] = *reinterpret_cast<const uint32_t*>(nrow + 4 * t);
+          nw[r][0] = *reinterpret_cast<const uint32_t*>(nr);
         }
       }
       float c1[QT][4], c2[QT][4];
@@ -780,11 +836,12 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         for (int r = 0; r < 2; ++r) {
           constexpr bool FAR = KB == 4 && !F32N;   // codes are unpacked four apart
           const int i0 = FAR ? 8 * (ks >> 2) + (ks & 3) : 2 * ks, i1 = FAR ? i0 + 4 : i0 + 1;
-          u[r] = *reinterpret_cast<const uint32_t*>(tk + ((pg_rotr(ca[r][i0 >> 2], (wk * (i0 & 3) - kTabShift) & 31) & km) | lane_off));
-          u[2 + r] = *reinterpret_cast<const uint32_t*>(tk + ((pg_rotr(ca[r][i1 >> 2], (wk * (i1 & 3) - kTabShift) & 31) & km) | lane_off));
+          const uint32_t mask = W ? ((1u << W) - 1u) << kTabShift : km;
+          u[r] = *reinterpret_cast<const uint32_t*>(tk + ((run[r].offset(i0, wk) & mask) | lane_off));
+          u[2 + r] = *reinterpret_cast<const uint32_t*>(tk + ((run[r].offset(i1, wk) & mask) | lane_off));
           uint32_t hb;
           if constexpr (F32N) {
-            const float2 v = *reinterpret_cast<const float2*>(nf[r] + 2 * ks);
+            const float2 v = *reinterpret_cast<const float2*>(nrow + 8 * r * knb + 8 * ks);
             hb = ab[r].x == 0.f ? 0u : h2_bits(__floats2half2_rn(v.x * ab[r].y, v.y * ab[r].y));
           } else if constexpr (LIN) {
             hb = KB == 8 ? __byte_perm(nw[r][(ks >> 1) % KW], 0u, (ks & 1) ? 0x4342 : 0x4140) : (nw[r][(ks >> 2) % KW] >> (4 * (ks & 3))) & 0x000F000Fu;
@@ -816,17 +873,19 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   // (cos, sin) goes in as it is.  w1, w2: the weights of this lane's tokens g, g + 8 of a tile (query
   // 4 x + t) as two halves; they are handed to the lanes that need them by shuffles.
   const uint32_t put0 = g & 1 ? 0x1044u : 0x4410u, put1 = g & 1 ? 0x3244u : 0x4432u;
-  auto values_mma = [&](const uint32_t (&w1)[QT][2], const uint32_t (&w2)[QT][2], auto nc_) {
-    constexpr int NC = decltype(nc_)::value;
+  auto values_mma = [&](const uint32_t (&w1)[QT][2], const uint32_t (&w2)[QT][2], auto nc_, auto w_) {
+    constexpr int NC = decltype(nc_)::value, W = decltype(w_)::value;
     constexpr bool F32N = NC == 4, LIN = NC == 0 || NC == 2;
     constexpr int VB = NC <= 1 ? 4 : 8;
     constexpr bool N16 = VB == 4 && VP == 4 && !F32N;    // a token's norms are 16 bits: two tokens in a word
     constexpr int VW = F32N ? 1 : (VP * VB + 31) / 32;
-    const int wv = p.v.w;
-    const int vbit = VP * g * wv, vsh = vbit & 31;       // a run starts at a byte (VP = 8) or half a byte
-    const uint8_t* const va = st_v + (vbit >> 5) * 4;
+    constexpr int vnb = F32N ? 4 * C::P : C::P * VB / 8;
+    const int wv = W ? W : p.v.w, vab = W ? C::P * W / 8 : p.v.ab, vbit = VP * g * wv;
+    const uint8_t* arow = st_v + t * vab + (vbit >> 5) * 4;
+    const uint8_t* nrow = st_vn + t * vnb + (F32N ? 4 * VP * g : VP * VB * g / 8);
+    const uint32_t* cst = vd + t;
 #pragma unroll 1
-    for (int hf = 0; hf < 2; ++hf) {
+    for (int hf = 0; hf < 2; ++hf, arow += kTile * vab, nrow += kTile * vnb, cst += kTile) {
       if ((hf ? b.valid1 : b.valid0) == 0) continue;
       uint32_t p1[QT][2], p2[QT][2];               // tokens t, t + 8 | t + 4, t + 12 of query g / 2
 #pragma unroll
@@ -840,28 +899,22 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         }
 #pragma unroll
       for (int s8 = 0; s8 < 2; ++s8) {
-        uint32_t ca[2][VP / 4], nw[2][VW], sl[2];
-        const float* nf[2] = {nullptr, nullptr};
-        float fs[2] = {0.f, 0.f};
+        Run<W, VP> run[2];
+        uint32_t nw[2][VW], sl[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int tok = kTile * hf + 8 * s8 + 4 * i + t;
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(va + tok * p.v.ab);
-          const uint32_t q0 = w[0], q1 = w[1];
-          ca[i][0] = __funnelshift_r(q0, q1, vsh);
-          if constexpr (VP == 8) ca[i][1] = __funnelshift_rc(ca[i][0], __funnelshift_r(q1, w[2], vsh), 4 * wv);
-          const uint8_t* nrow = st_vn + tok * p.v.nb;
-          sl[i] = vd[tok];
+          const int row = 8 * s8 + 4 * i;          // of this tile, behind token t
+          run[i].load(arow + row * vab, vbit & 31, wv);
+          const uint8_t* nr = nrow + row * vnb;
+          sl[i] = cst[row];
           if constexpr (F32N) {
-            nf[i] = reinterpret_cast<const float*>(nrow) + VP * g;
-            fs[i] = __uint_as_float(sl[i]);
           } else if constexpr (VW == 2) {
-            const uint2 v = *reinterpret_cast<const uint2*>(nrow + 8 * g);
+            const uint2 v = *reinterpret_cast<const uint2*>(nr);
             nw[i][0] = v.x; nw[i][1] = v.y;
           } else if constexpr (N16) {
-            nw[i][0] = *reinterpret_cast<const uint16_t*>(nrow + 2 * g);
+            nw[i][0] = *reinterpret_cast<const uint16_t*>(nr);
           } else {
-            nw[i][0] = *reinterpret_cast<const uint32_t*>(nrow + 4 * g);
+            nw[i][0] = *reinterpret_cast<const uint32_t*>(nr);
           }
         }
         if constexpr (N16) {                       // (token 0, token 1) of a position in one pair of halves
@@ -877,11 +930,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
           uint32_t u[4], y[4], hb[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            u[2 * i] = *reinterpret_cast<const uint32_t*>(tv + ((pg_rotr(ca[i][j0 >> 2], (wv * (j0 & 3) - kTabShift) & 31) & vm) | lane_off));
-            u[2 * i + 1] = *reinterpret_cast<const uint32_t*>(tv + ((pg_rotr(ca[i][j1 >> 2], (wv * (j1 & 3) - kTabShift) & 31) & vm) | lane_off));
+            const uint32_t mask = W ? ((1u << W) - 1u) << kTabShift : vm;
+            u[2 * i] = *reinterpret_cast<const uint32_t*>(tv + ((run[i].offset(j0, wv) & mask) | lane_off));
+            u[2 * i + 1] = *reinterpret_cast<const uint32_t*>(tv + ((run[i].offset(j1, wv) & mask) | lane_off));
             if constexpr (F32N) {
-              const float2 v = *reinterpret_cast<const float2*>(nf[i] + 2 * m);
-              hb[i] = fs[i] == 0.f ? 0u : h2_bits(__floats2half2_rn(v.x * fs[i], v.y * fs[i]));
+              const float2 v = *reinterpret_cast<const float2*>(nrow + (8 * s8 + 4 * i) * vnb + 8 * m);
+              const float f = __uint_as_float(sl[i]);
+              hb[i] = f == 0.f ? 0u : h2_bits(__floats2half2_rn(v.x * f, v.y * f));
             } else if constexpr (N16) {
               const int j = i ? j1 : j0;
               if constexpr (LIN) hb[i] = (nw[0][0] >> (4 * j)) & 0x000F000Fu;
@@ -1034,16 +1089,20 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         kc[lane] = k2;
         __syncwarp();
         switch (p.k.nc) {
-          case 0: scores_mma(sv, IC<0>{}); break;
-          case 1: scores_mma(sv, IC<1>{}); break;
-          case 2: scores_mma(sv, IC<2>{}); break;
-          case 3: scores_mma(sv, IC<3>{}); break;
-          default: scores_mma(sv, IC<4>{}); break;
+          case 0: scores_mma(sv, IC<0>{}, IC<0>{}); break;
+          case 1: scores_mma(sv, IC<1>{}, IC<0>{}); break;
+          case 2:                                  // the usual keys: 8-bit linear norms
+            if (p.k.w == 6) scores_mma(sv, IC<2>{}, IC<6>{});
+            else if (p.k.w == 8) scores_mma(sv, IC<2>{}, IC<8>{});
+            else scores_mma(sv, IC<2>{}, IC<0>{});
+            break;
+          case 3: scores_mma(sv, IC<3>{}, IC<0>{}); break;
+          default: scores_mma(sv, IC<4>{}, IC<0>{}); break;
         }
       }
       __syncwarp();                                // every lane is done with the K rows
     }
-    if (more) issue(false, nx);
+    if (more) issue(p.k, stage_k, bar_k, nx);
     if constexpr (EXACT) {
       if (any) {
         bool moved = false;
@@ -1164,16 +1223,23 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
           }
         }
         switch (p.v.nc) {
-          case 0: values_mma(w1, w2, IC<0>{}); break;
-          case 1: values_mma(w1, w2, IC<1>{}); break;
-          case 2: values_mma(w1, w2, IC<2>{}); break;
-          case 3: values_mma(w1, w2, IC<3>{}); break;
-          default: values_mma(w1, w2, IC<4>{}); break;
+          case 0: values_mma(w1, w2, IC<0>{}, IC<0>{}); break;
+          case 1:                                  // the usual values: 4-bit norms in log space
+            if (p.v.w == 6) values_mma(w1, w2, IC<1>{}, IC<6>{});
+            else if (p.v.w == 8) values_mma(w1, w2, IC<1>{}, IC<8>{});
+            else values_mma(w1, w2, IC<1>{}, IC<0>{});
+            break;
+          case 2:
+            if (p.v.w == 6) values_mma(w1, w2, IC<2>{}, IC<6>{});
+            else values_mma(w1, w2, IC<2>{}, IC<0>{});
+            break;
+          case 3: values_mma(w1, w2, IC<3>{}, IC<0>{}); break;
+          default: values_mma(w1, w2, IC<4>{}, IC<0>{}); break;
         }
         __syncwarp();                              // every lane is done with the V rows
       }
     }
-    if (more) issue(true, nx);
+    if (more) issue(p.v, stage_v, bar_v, nx);
     if (b.ends) {
       // the part's record, elements in their order; in the place of the queries, unless the
       // part began in an earlier warp

@@ -614,13 +614,17 @@ def launch_count(jobs) -> int:
 # ---------------------------------------------------------------------------
 _PAGING_FMT = struct.Struct("=QqiiQqii")
 _BOXES_FMT = struct.Struct("=QQi4x")
-_ATT_PAGES_FMT = struct.Struct("=32s32sQQQQq48sQQiiifQqqQqq")
+_ATT_PAGES_FMT = struct.Struct("=32s32sQQQQq48sQQiiifQqqQqq")   # tac_attend_pages_args
+_ATT_HEAD_FMT = struct.Struct("=32s32sQQQQq")                     # its first fields: what a PagedCache holds
+_ATT_TAIL_FMT = struct.Struct("=QqiiQqiiQQiiifQqqQqq")            # the others, paging spelled out
+assert _ATT_HEAD_FMT.size + _ATT_TAIL_FMT.size == _ATT_PAGES_FMT.size
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedCache:
-    """Record pools of one layer: `pages` pages of page_tokens tokens of each KV head.  The
-    record slot of (page p, head h, offset o) is (p * kv_heads + h) * page_tokens + o."""
+    """Record pools of one layer: pages of page_tokens tokens of each KV head.  The record slot of
+    (page p, head h, offset o) is (p * kv_heads + h) * page_tokens + o.  A handle: the planes'
+    addresses and the codebooks are taken at its first use."""
     k: Cache
     v: Cache
     kv_heads: int
@@ -650,11 +654,20 @@ class PagedCache:
         s = (page[:, None] * self.kv_heads + head) * self.page_tokens + (pos % self.page_tokens)[:, None]
         return s.reshape(-1)
 
+    def _handle(self):
+        """(packed codebooks, planes and capacity; pages; d; the planes, held)."""
+        k, v = self.k, self.v
+        planes = (k.codes, k.norms, v.codes, v.norms)
+        got = (_ATT_HEAD_FMT.pack(_cfg_bytes(k.cfg), _cfg_bytes(v.cfg), *(t.data_ptr() for t in planes), k.capacity),
+               self.pages, k.cfg.d, planes)
+        self.__dict__["_packed"] = got
+        return got
 
-@dataclass
+
+@dataclass(frozen=True)
 class PageBounds:
     """The boxes of a paged cache's keys (tac_page_boxes): lo_j 2^e <= k_tj <= hi_j 2^e over each
-    (page, head)'s tokens."""
+    (page, head)'s tokens.  A handle: the tensors' addresses are taken at its first use."""
     codes: object        # int8 [pages, kv_heads, 2, d]: lo, hi
     scales: object       # float32 [pages, kv_heads]: 2^e (inf: a key is not finite)
     page_tokens: int
@@ -665,55 +678,66 @@ class PageBounds:
         return PageBounds(torch.zeros((pages, kv_heads, 2, d), dtype=torch.int8, device=device),
                           torch.zeros((pages, kv_heads), dtype=torch.float32, device=device), page_tokens)
 
-    def _checked(self):
+    def _handle(self):
+        """(packed boxes, pages, KV heads, d)."""
         torch = _torch()
         c, s = self.codes, self.scales
         if c.dtype != torch.int8 or c.dim() != 4 or c.shape[2] != 2 or not c.is_contiguous() or not c.is_cuda:
             raise ValueError("bounds.codes: a contiguous int8 [pages, kv_heads, 2, d] device tensor")
         if s.dtype != torch.float32 or s.shape != c.shape[:2] or not s.is_contiguous() or not s.is_cuda:
             raise ValueError("bounds.scales: a contiguous float32 [pages, kv_heads] device tensor")
-        return c.shape
+        pages, heads, _, d = c.shape
+        got = (_BOXES_FMT.pack(c.data_ptr(), s.data_ptr(), d), pages, heads, d)
+        self.__dict__["_packed"] = got
+        return got
 
 
-def _int32(t, shape, name):
+def _int32(t, shape, name, torch):
     """Address of a contiguous int32 device tensor of this shape."""
-    torch = _torch()
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name}: a contiguous int32 {list(shape)} device tensor, got {t.dtype} {list(t.shape)}")
     return t.data_ptr()
 
 
-def _paging_bytes(table, lengths, pages: int, kv_heads: int, page_tokens: int) -> bytes:
-    torch = _torch()
-    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError("page_table: an int32 [seqs, pages of a sequence] device tensor with unit inner stride")
-    seqs, width = table.shape
-    stride = table.stride(0) if seqs > 1 else width
-    return _PAGING_FMT.pack(table.data_ptr(), max(stride, width), width, seqs,
-                            0 if lengths is None else _int32(lengths, (seqs,), "lengths"), pages, kv_heads, page_tokens)
+def _table(t, torch):
+    """(address, row stride, columns, sequences) of a page table."""
+    shape = t.shape
+    if t.dtype is not torch.int32 or len(shape) != 2 or not t.is_cuda:
+        raise ValueError("page_table: an int32 [seqs, pages of a sequence] device tensor")
+    seqs, width = shape
+    stride, inner = t.stride()
+    if width > 1 and inner != 1:
+        raise ValueError("page_table: unit inner stride")
+    return t.data_ptr(), (stride if seqs > 1 and stride > width else width), width, seqs
 
 
-def _groups(q, seqs: int, kv_heads: int, d: int, name: str):
+def _groups(q, seqs: int, heads: int, d: int, name: str, torch):
     """(address, dtype code, group, sequence stride, row stride) of a [seqs, heads * group, d] tensor."""
-    if q.dim() != 3 or q.shape[0] != seqs or q.shape[2] != d or q.shape[1] % kv_heads or not q.is_cuda or q.stride(2) != 1:
-        raise ValueError(f"{name}: a [{seqs}, query heads (a multiple of {kv_heads}), {d}] device tensor with unit inner "
-                         f"stride, got {tuple(q.shape)}")
-    return q.data_ptr(), _dtype_code(q), q.shape[1] // kv_heads, q.stride(0), q.stride(1)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or shape[0] != seqs or shape[2] != d or shape[1] % heads or not q.is_cuda:
+        raise ValueError(f"{name}: a [{seqs}, query heads (a multiple of {heads}), {d}] device tensor, got {tuple(shape)}")
+    s_seq, s_row, inner = q.stride()
+    if inner != 1:
+        raise ValueError(f"{name}: unit inner stride")
+    return q.data_ptr(), (BF16 if dtype is torch.bfloat16 else _dtype_code(q)), shape[1] // heads, s_seq, s_row
 
 
 def page_bounds(bounds: PageBounds, k, page_table, start, first=None, stream=None) -> None:
     """tac_page_bounds: brings the boxes up to date with keys just written.  k [rows, kv_heads, d]
     (bf16 or fp32): rows first[s] .. first[s + 1] - 1 (first: int32 [seqs + 1]) are the keys of sequence s
     at positions start[s] (int32 [seqs]) and on; without `first` one row for each sequence."""
-    pages, heads, _, d = bounds._checked()
-    if k.dim() != 3 or k.shape[1] != heads or k.shape[2] != d or not k.is_cuda or k.stride(2) != 1:
-        raise ValueError(f"k: a [rows, {heads}, {d}] device tensor with unit inner stride, got {tuple(k.shape)}")
-    seqs = page_table.shape[0]
-    _check(load().tac_page_bounds(
-        _BOXES_FMT.pack(bounds.codes.data_ptr(), bounds.scales.data_ptr(), d),
-        _paging_bytes(page_table, None, pages, heads, bounds.page_tokens), k.data_ptr(), _dtype_code(k), k.shape[0],
-        k.stride(0), k.stride(1), None if first is None else _int32(first, (seqs + 1,), "first"),
-        _int32(start, (seqs,), "start"), _stream_ptr(stream)))
+    torch = _torch()
+    boxes, pages, heads, d = bounds.__dict__.get("_packed") or bounds._handle()
+    shape = k.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d or not k.is_cuda or k.stride(2) != 1:
+        raise ValueError(f"k: a [rows, {heads}, {d}] device tensor with unit inner stride, got {tuple(shape)}")
+    t_ptr, t_stride, width, seqs = _table(page_table, torch)
+    rc = load().tac_page_bounds(
+        boxes, _PAGING_FMT.pack(t_ptr, t_stride, width, seqs, 0, pages, heads, bounds.page_tokens), k.data_ptr(),
+        _dtype_code(k), shape[0], k.stride(0), k.stride(1), None if first is None else _int32(first, (seqs + 1,), "first", torch),
+        _int32(start, (seqs,), "start", torch), _stream_ptr(stream))
+    if rc:
+        _check(rc)
 
 
 def select_pages(q, bounds: PageBounds, page_table, lengths, budget: int, keep_first: int = 1, keep_last: int = 1,
@@ -723,10 +747,9 @@ def select_pages(q, bounds: PageBounds, page_table, lengths, budget: int, keep_f
     among them.  Returns (selected int32 [seqs, kv_heads, budget], ascending, then -1; counts int32
     [seqs, kv_heads]), written to `selected` and `counts` where given."""
     torch = _torch()
-    pages, heads, _, d = bounds._checked()
-    seqs = page_table.shape[0]
-    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q")
-    paging = _paging_bytes(page_table, lengths, pages, heads, bounds.page_tokens)
+    boxes, pages, heads, d = bounds.__dict__.get("_packed") or bounds._handle()
+    t_ptr, t_stride, width, seqs = _table(page_table, torch)
+    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q", torch)
     made = []
     if selected is None:
         selected = torch.empty((seqs, heads, max(budget, 0)), dtype=torch.int32, device=q.device)
@@ -734,10 +757,14 @@ def select_pages(q, bounds: PageBounds, page_table, lengths, budget: int, keep_f
     if counts is None:
         counts = torch.empty((seqs, heads), dtype=torch.int32, device=q.device)
         made.append(counts)
-    _check(load().tac_select_pages(
-        _BOXES_FMT.pack(bounds.codes.data_ptr(), bounds.scales.data_ptr(), d), paging, ptr, dt, group, s_seq, s_row, budget,
-        keep_first, keep_last, _int32(selected, (seqs, heads, budget), "selected"), _int32(counts, (seqs, heads), "counts"),
-        _stream_ptr(stream)))
+    rc = load().tac_select_pages(
+        boxes, _PAGING_FMT.pack(t_ptr, t_stride, width, seqs, _int32(lengths, (seqs,), "lengths", torch), pages, heads,
+                                bounds.page_tokens),
+        ptr, dt, group, s_seq, s_row, budget, keep_first, keep_last,
+        _int32(selected, (seqs, heads, budget), "selected", torch), _int32(counts, (seqs, heads), "counts", torch),
+        _stream_ptr(stream))
+    if rc:
+        _check(rc)
     if stream is not None:
         for t in made:
             t.record_stream(stream)   # in use on `stream` until its work is done
@@ -750,30 +777,32 @@ def attend_pages(q, cache: PagedCache, page_table, lengths, scale: float, select
     all tokens of each sequence, or over the pages that select_pages chose (`selected`, `counts`).  Allocates
     the output and the workspace (torch) where none is given; returns the output."""
     torch = _torch()
-    heads, d = cache.kv_heads, cache.k.cfg.d
-    seqs = page_table.shape[0]
-    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q")
+    head, pages, d, _ = cache.__dict__.get("_packed") or cache._handle()
+    heads = cache.kv_heads
+    t_ptr, t_stride, width, seqs = _table(page_table, torch)
+    ptr, dt, group, s_seq, s_row = _groups(q, seqs, heads, d, "q", torch)
     made = []
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         made.append(out)
-    o_ptr, o_dt, o_group, o_seq, o_row = _groups(out, seqs, heads, d, "out")
-    if o_dt != dt or o_group != group:
-        raise ValueError("out must match q in shape and dtype")
+        o_ptr, o_row = out.data_ptr(), d
+        o_seq = o_row * heads * group
+    else:
+        o_ptr, o_dt, o_group, o_seq, o_row = _groups(out, seqs, heads, d, "out", torch)
+        if o_dt != dt or o_group != group:
+            raise ValueError("out must match q in shape and dtype")
     budget, sel_ptr, cnt_ptr = 0, 0, 0
-    if (selected is None) != (counts is None):
-        raise ValueError("selected and counts come together")
-    if selected is not None:
-        if selected.dim() != 3:
+    if selected is not None and counts is not None:
+        if len(selected.shape) != 3:
             raise ValueError("selected: an int32 [seqs, kv_heads, budget] tensor")
         budget = selected.shape[2]
-        sel_ptr = _int32(selected, (seqs, heads, budget), "selected")
-        cnt_ptr = _int32(counts, (seqs, heads), "counts")
-    args = _ATT_PAGES_FMT.pack(
-        _cfg_bytes(cache.k.cfg), _cfg_bytes(cache.v.cfg), cache.k.codes.data_ptr(), cache.k.norms.data_ptr(),
-        cache.v.codes.data_ptr(), cache.v.norms.data_ptr(), cache.k.capacity,
-        _paging_bytes(page_table, lengths, cache.pages, heads, cache.page_tokens), sel_ptr, cnt_ptr, budget, dt, group,
-        scale, ptr, s_seq, s_row, o_ptr, o_seq, o_row)
+        sel_ptr = _int32(selected, (seqs, heads, budget), "selected", torch)
+        cnt_ptr = _int32(counts, (seqs, heads), "counts", torch)
+    elif selected is not None or counts is not None:
+        raise ValueError("selected and counts come together")
+    args = head + _ATT_TAIL_FMT.pack(
+        t_ptr, t_stride, width, seqs, _int32(lengths, (seqs,), "lengths", torch), pages, heads, cache.page_tokens,
+        sel_ptr, cnt_ptr, budget, dt, group, scale, ptr, s_seq, s_row, o_ptr, o_seq, o_row)
     lib = load()
     if workspace is None:
         need = lib.tac_attend_pages_workspace_bytes(args)
@@ -781,7 +810,12 @@ def attend_pages(q, cache: PagedCache, page_table, lengths, scale: float, select
             raise TacError(TAC_E_INVAL, last_error())
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         made.append(workspace)
-    _check(lib.tac_attend_pages(args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+        size = need
+    else:
+        size = workspace.numel() * workspace.element_size()
+    rc = lib.tac_attend_pages(args, workspace.data_ptr(), size, _stream_ptr(stream))
+    if rc:
+        _check(rc)
     if stream is not None:
         for t in made:
             t.record_stream(stream)   # in use on `stream` until its work is done

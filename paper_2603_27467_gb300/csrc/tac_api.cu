@@ -1131,8 +1131,9 @@ int check_attend_pages(const tac_attend_pages_args* A, const char* who) {
   // tiles, their total and the second kernel's grid are 32-bit numbers
   const int64_t per = g.page_tokens / tac::kTile, segs = (int64_t)g.seqs * g.kv_heads;
   const int64_t cols = A->selected ? A->budget : g.table_pages;
-  if (cols * per > 0x7fffffff || (segs > 0 && cols * per > 0x7fffffff / segs) || segs * A->group > 0x7fffffff)
-    return fail(TAC_E_UNSUPPORTED, "%s: more than 2^31 - 1 tiles of 16 tokens in one call", who);
+  constexpr int64_t kMost = (int64_t)1 << 30;
+  if (cols * per > kMost || (segs > 0 && cols * per > kMost / segs) || segs * A->group > kMost)
+    return fail(TAC_E_UNSUPPORTED, "%s: more than 2^30 tiles of 16 tokens in one call", who);
   if (segs == 0) return TAC_OK;
   if (g.pages > 0 && (!A->k_codes || !A->k_norms || !A->v_codes || !A->v_norms || !aligned16(A->k_codes) ||
                       !aligned16(A->k_norms) || !aligned16(A->v_codes) || !aligned16(A->v_norms)))
@@ -1142,11 +1143,11 @@ int check_attend_pages(const tac_attend_pages_args* A, const char* who) {
   return rc;
 }
 
-// Workspace: the plan (items + 2 words), then the parts of every CTA.
+// Workspace: the plan (items + 3 words), then the parts of every CTA.
 int attend_pages_items(const tac_attend_pages_args* A) {
   return A->selected ? A->paging.seqs * A->paging.kv_heads : A->paging.seqs;
 }
-int64_t attend_pages_plan_bytes(const tac_attend_pages_args* A) { return (4 * ((int64_t)attend_pages_items(A) + 2) + 15) & ~(int64_t)15; }
+int64_t attend_pages_plan_bytes(const tac_attend_pages_args* A) { return (4 * ((int64_t)attend_pages_items(A) + 3) + 15) & ~(int64_t)15; }
 int64_t attend_pages_bytes(const tac_attend_pages_args* A, int ctas) {
   return attend_pages_plan_bytes(A) + (int64_t)ctas * 2 * A->group * tac::pg_rec_floats(A->cfg_k.d) * 4;
 }

@@ -122,7 +122,7 @@ __device__ __forceinline__ void pg_fwht(float (&y)[D / 32], int lane) {
   }
 }
 
-// Row a of a (sequence, head)'s queries, rotated and times scale * log2(e): elements E lane + k.
+// Row a of a (sequence, head)'s queries: elements E lane + k.
 template <int D>
 __device__ __forceinline__ void pg_load_query(const AttPagesParams& p, bool bf, int seq, int head, int a, int lane,
                                               float (&y)[D / 32]) {
@@ -145,6 +145,11 @@ __device__ __forceinline__ void pg_load_query(const AttPagesParams& p, bool bf, 
       y[2 * k + 1] = w.y;
     }
   }
+}
+// It rotated, times scale * log2(e).
+template <int D>
+__device__ __forceinline__ void pg_turn_query(const AttPagesParams& p, int lane, float (&y)[D / 32]) {
+  constexpr int E = D / 32;
   const uint32_t sg = p.k.signs[(E * lane) >> 5] >> ((E * lane) & 31);
 #pragma unroll
   for (int k = 0; k < E; ++k)
@@ -198,7 +203,7 @@ __device__ __forceinline__ int pg_tiles(const AttPagesParams& p, int i) {
 // Walks a warp's tiles in order, two (a batch) at a time.  The places of up to 32 batches are
 // worked out at once, one a lane, and handed out by shuffles.
 struct Cursor {
-  int64_t left;          // tiles still to come, behind the window
+  int left;              // tiles still to come, behind the window
   int item, head, seq;   // the (sequence, head) of the window
   int i, nt;             // the tile behind the window, the (sequence, head)'s tiles
   int j, n;              // next batch of the window, its batches
@@ -245,7 +250,7 @@ __device__ __forceinline__ void cursor_fill(const AttPagesParams& p, Cursor& c, 
     c.head = c.item - c.seq * p.pg.heads;
   }
   const int len = pg_len(p, c.seq);
-  const int m = (int)min(c.left, (int64_t)(c.nt - c.i)), take = min(m, 64);
+  const int m = min(c.left, c.nt - c.i), take = min(m, 64);
   uint32_t v0 = 0, v1 = 0;
   c.t0 = c.t1 = 0;
   if (2 * lane < take) cursor_tile(p, c, len, c.i + 2 * lane, c.t0, v0);
@@ -309,7 +314,7 @@ __host__ __device__ inline int pg_stage_bytes(const Book& b) { return kBatch * (
 // CTA-wide bookkeeping, in front of the dynamic shared memory.
 struct PgShared {
   int64_t bars[2 * kMaxWarps];                     // mbarriers: K, V of each warp
-  int pref[kMaxWarps * 32 + 1];                    // first tile of each thread's items
+  int pref[kMaxWarps * 32];                        // first tile of each thread's items
   int scan[kMaxWarps];
   // parts: what each warp left.  0: one that began in an earlier warp, 1: one that begins
   // here and goes on.  -1: none; seq * heads + head otherwise.
@@ -318,49 +323,65 @@ struct PgShared {
   int empty[kMaxWarps];                            // no tiles
 };
 
-// Joins of a CTA's parts: every (part that begins a chain, query) is one warp's task.
-// rec(w, which): the record of a warp's part.
+// Joins of a CTA's parts: every (chain of parts, query) is one warp's task.  A chain starts with a part
+// that begins in its warp, or with the CTA's first part, and goes on through the warps whose first
+// part continues it.  rec(w, which): the record of a warp's part.
 template <int D, typename Rec>
 __device__ __forceinline__ void pg_join(const AttPagesParams& p, const PgShared& sh, bool bf, int nw, int warp, int lane,
                                         Rec rec) {
-  constexpr int E = D / 32;
+  constexpr int E = D / 32, RF = pg_rec_floats(D);
+  const bool live = lane < nw && !sh.empty[lane];
+  const int id0 = live ? sh.part[lane][0] : -1, id1 = live ? sh.part[lane][1] : -1;
+  const uint32_t has0 = __ballot_sync(0xffffffffu, id0 >= 0), has1 = __ballot_sync(0xffffffffu, id1 >= 0);
+  const uint32_t ends = __ballot_sync(0xffffffffu, id0 >= 0 && sh.ends0[lane]);
+  const uint32_t busy = __ballot_sync(0xffffffffu, live);
+  uint32_t lead0 = has0 & busy & (0u - busy), lead1 = has1;   // of the first warp with tiles, if it continues a part
   int task = 0;
-  for (int lead = 0; lead < 2 * nw; ++lead) {
-    const int w0 = lead >> 1, which = lead & 1, id = sh.part[w0][which];
-    if (id < 0) continue;
-    if (which == 0) {                              // only the CTA's first part can have begun before it
-      bool before = false;
-      for (int w = 0; w < w0; ++w) before |= !sh.empty[w];
-      if (before) continue;
+  while (lead0 | lead1) {
+    const int which = lead0 ? 0 : 1, w0 = __ffs(which ? lead1 : lead0) - 1;
+    if (which) lead1 &= lead1 - 1; else lead0 = 0;
+    uint32_t chain = has0 & (0xFFFFFFFEu << w0);   // the parts that may continue it
+    bool ended = which == 0 && ((ends >> w0) & 1u);
+    if (ended) {
+      chain = 0;
+    } else if (ends & chain) {
+      chain &= (2u << (__ffs(ends & chain) - 1)) - 1u;
+      ended = true;
     }
-    int w1 = w0;                                   // the last warp of the chain
-    bool ended = which == 0 && sh.ends0[w0];
-    for (int w = w0 + 1; w < nw && !ended; ++w) {
-      if (sh.empty[w]) continue;
-      w1 = w;
-      ended = sh.ends0[w];
-    }
-    const bool whole = which == 1 && ended;
+    chain |= 1u << w0;
+    const int id = __shfl_sync(0xffffffffu, which ? id1 : id0, w0);
+    const bool mine = (chain >> lane) & 1u;
     for (int a = 0; a < p.group; ++a, ++task) {
       if (task % nw != warp) continue;
-      float M = -INFINITY;
-      for (int w = w0; w <= w1; ++w)
-        if (!sh.empty[w]) M = fmaxf(M, rec(w, w == w0 ? which : 0)[a * pg_rec_floats(D)]);
-      float l = 0.f, y[E];
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (mine) ml = *reinterpret_cast<const float2*>(rec(lane, lane == w0 ? which : 0) + a * RF);
+      float M = ml.x;
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
+      float l = f * ml.y;
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      float y[E];
 #pragma unroll
       for (int k = 0; k < E; ++k) y[k] = 0.f;
+      const int w1 = 31 - __clz(chain);
+#pragma unroll 4
       for (int w = w0; w <= w1; ++w) {
-        if (sh.empty[w]) continue;
-        const float* r = rec(w, w == w0 ? which : 0) + a * pg_rec_floats(D);
-        const float f = r[0] == -INFINITY ? 0.f : ex2_approx(r[0] - M);
-        l = __fmaf_rn(r[1], f, l);
+        const float fw = __shfl_sync(0xffffffffu, f, w);
+        if (fw == 0.f) continue;
+        const float2* r = reinterpret_cast<const float2*>(rec(w, w == w0 ? which : 0) + a * RF + 2 + E * lane);
 #pragma unroll
-        for (int k = 0; k < E; ++k) y[k] = __fmaf_rn(r[2 + E * lane + k], f, y[k]);
+        for (int k = 0; k < E; k += 2) {
+          const float2 v = r[k / 2];
+          y[k] = __fmaf_rn(v.x, fw, y[k]);
+          y[k + 1] = __fmaf_rn(v.y, fw, y[k + 1]);
+        }
       }
-      if (whole) {
+      if (which == 1 && ended) {
         pg_store_out<D>(p, bf, id / p.pg.heads, id % p.pg.heads, a, lane, y, l);
       } else {
-        float* out = p.part + (((int64_t)blockIdx.x * 2 + which) * p.group + a) * pg_rec_floats(D);
+        float* out = p.part + (((int64_t)blockIdx.x * 2 + which) * p.group + a) * RF;
         if (lane == 0) *reinterpret_cast<float2*>(out) = make_float2(M, l);
 #pragma unroll
         for (int k = 0; k < E; k += 2) *reinterpret_cast<float2*>(out + 2 + E * lane + k) = make_float2(y[k], y[k + 1]);
@@ -369,63 +390,96 @@ __device__ __forceinline__ void pg_join(const AttPagesParams& p, const PgShared&
   }
 }
 
-// The plan of a CTA: total tiles, and the warp's cursor.  All threads call it.
-__device__ __forceinline__ int64_t pg_plan(const AttPagesParams& p, PgShared& sh, int nw, Cursor& c) {
+// The plan of a CTA: total tiles, and the warp's cursor.  All threads call it.  Warp w of the W in use
+// starts at tile floor(total w / W).
+__device__ __forceinline__ int pg_start(int total, int w, int W) {
+  const int q = total / W, r = total - q * W;
+  return q * w + (int)((uint32_t)(r * w) / (uint32_t)W);       // r w < W^2, W <= 16 * kAttPgMaxCtas
+}
+static_assert((int64_t)kMaxWarps * kAttPgMaxCtas * kMaxWarps * kAttPgMaxCtas < (int64_t)1 << 31, "pg_start");
+__device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, int nw, Cursor& c) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = nw * 32;
   const int items = p.items, mult = p.selected ? 1 : p.pg.heads;
-  const int chunk = (items + nt - 1) / nt;
-  int mine = 0;
-  for (int i = tid * chunk; i < min(items, (tid + 1) * chunk); ++i) mine += pg_tiles(p, i) * mult;
+  const bool few = items <= 32;                    // every warp by itself, an item a lane
+  const int chunk = few ? 1 : (items + nt - 1) / nt;
+  int mine = 0;                                    // tiles of this lane's (thread's) items
+  if (few) {
+    if (lane < items) mine = pg_tiles(p, lane) * mult;
+  } else {
+    for (int i = tid * chunk; i < min(items, (tid + 1) * chunk); ++i) mine += pg_tiles(p, i) * mult;
+  }
   int x = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 31) sh.scan[warp] = x;
-  __syncthreads();
-  int before = 0;
-  for (int w = 0; w < warp; ++w) before += sh.scan[w];
-  sh.pref[tid] = before + x - mine;
-  if (tid == nt - 1) sh.pref[nt] = before + x;
-  __syncthreads();
-  const int64_t total = sh.pref[nt];
-  // at least two tiles a warp
-  const int64_t nc = min((int64_t)p.ctas, (total + 2 * nw - 1) / (2 * nw));
-  if (blockIdx.x == 0) {                           // for the second kernel
-    int at = sh.pref[tid];
-    for (int i = tid * chunk; i < min(items, (tid + 1) * chunk); ++i) {
-      p.plan[i] = at;
-      at += pg_tiles(p, i) * mult;
+  int total, at = x - mine;                        // first tile of the lane's (thread's) items
+  if (few) {
+    total = __shfl_sync(0xffffffffu, x, 31);
+  } else {
+    if (lane == 31) sh.scan[warp] = x;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < nw; ++w) {
+      if (w == warp) at += total;
+      total += sh.scan[w];
     }
-    if (tid == 0) {
-      p.plan[items] = (int)total;
-      p.plan[items + 1] = (int)nc;
+    sh.pref[tid] = at;
+    __syncthreads();
+  }
+  // at least two tiles a warp, and all CTAs before many warps of each
+  const int warps = min(nw, max(1, (total + 2 * p.ctas - 1) / (2 * p.ctas)));
+  const int nc = min(p.ctas, (total + 2 * warps - 1) / (2 * warps)), W = nc * warps;
+  if (blockIdx.x == 0 && (!few || warp == 0)) {    // for the second kernel
+    const int who = few ? lane : tid;
+    if (few) {
+      if (lane < items) p.plan[lane] = at;
+    } else {
+      int first = at;
+      for (int i = who * chunk; i < min(items, (who + 1) * chunk); ++i) {
+        p.plan[i] = first;
+        first += pg_tiles(p, i) * mult;
+      }
+    }
+    if (who == 0) {
+      p.plan[items] = total;
+      p.plan[items + 1] = nc;
+      p.plan[items + 2] = warps;
     }
   }
   c.left = 0;
   c.j = c.n = 0;
-  if ((int64_t)blockIdx.x >= nc) return 0;
-  const int64_t W = nc * nw, me = (int64_t)blockIdx.x * nw + warp;
-  int64_t t0 = total * me / W;
-  c.left = total * (me + 1) / W - t0;
-  if (c.left <= 0) return total;
-  int lo = 0, hi = nt - 1;                         // the thread whose items hold tile t0
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (sh.pref[mid] <= t0) lo = mid; else hi = mid - 1;
-  }
-  t0 -= sh.pref[lo];
-  int i = lo * chunk, n = pg_tiles(p, i);
-  while (t0 >= (int64_t)n * mult) {
-    t0 -= (int64_t)n * mult;
-    n = pg_tiles(p, ++i);
+  if ((int)blockIdx.x >= nc) return false;
+  if (warp >= warps) return true;
+  const int me = (int)blockIdx.x * warps + warp;
+  int t0 = pg_start(total, me, W);
+  c.left = pg_start(total, me + 1, W) - t0;
+  if (c.left <= 0) return true;
+  int i, n;
+  if (few) {
+    i = __ffs(__ballot_sync(0xffffffffu, x > t0)) - 1;
+    t0 -= __shfl_sync(0xffffffffu, at, i);
+    n = __shfl_sync(0xffffffffu, mine, i) / mult;
+  } else {
+    int lo = 0, hi = nt - 1;                       // the thread whose items hold tile t0
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sh.pref[mid] <= t0) lo = mid; else hi = mid - 1;
+    }
+    t0 -= sh.pref[lo];
+    i = lo * chunk;
+    n = pg_tiles(p, i);
+    while (t0 >= n * mult) {
+      t0 -= n * mult;
+      n = pg_tiles(p, ++i);
+    }
   }
   c.item = i;
   c.nt = n;
-  c.head = (int)(t0 / n);
-  c.i = (int)(t0 - (int64_t)c.head * n);
-  return total;
+  c.head = t0 / n;
+  c.i = t0 - c.head * n;
+  return true;
 }
 
 // (A, B) of one token: r^ = A c + B for the norm code c (log: its log2).  fp32 norms: A tells
@@ -567,7 +621,6 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     return reinterpret_cast<float*>(pool + w * warp_bytes + (which ? C::W_Q : C::W_REC));
   };
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t bar_k = pg_smem(&sh.bars[2 * warp]), bar_v = bar_k + 8;
   if (lane == 0) {
     pg_bar_init(bar_k);
@@ -577,8 +630,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     sh.ends0[warp] = 0;
   }
   Cursor cur;
-  const int64_t total = pg_plan(p, sh, nw, cur);
-  if (total == 0) return;                          // no tile for this CTA
+  if (!pg_plan(p, sh, nw, cur)) return;            // no tile for this CTA
   if (lane == 0) sh.empty[warp] = cur.left <= 0;
 
   // ---- staging: one lane (elected, so that the compiler knows it is one) copies the planes (angle | norm | header) of a batch's tiles, both at
@@ -996,11 +1048,19 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
       begun = b.first;
       __syncwarp();
 #pragma unroll 1
-      for (int a = 0; a < NQ; ++a) {
-        float y[E];
+      for (int a0 = 0; a0 < NQ; a0 += 4) {
+      float yy[4][E];                              // four rows at a time: their loads overlap
 #pragma unroll
-        for (int k = 0; k < E; ++k) y[k] = 0.f;
-        if (a < p.group) pg_load_query<D>(p, bf, b.seq, b.head, a, lane, y);
+      for (int a = 0; a < 4; ++a) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) yy[a][k] = 0.f;
+        if (a0 + a < p.group) pg_load_query<D>(p, bf, b.seq, b.head, a0 + a, lane, yy[a]);
+      }
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        const int a = a0 + a4;
+        float (&y)[E] = yy[a4];
+        pg_turn_query<D>(p, lane, y);
         if constexpr (EXACT) {
 #pragma unroll
           for (int k = 0; k < E; k += 2) {         // pair (E lane + k) / 2
@@ -1030,6 +1090,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
             w[16] = h2_bits(__floats2half2_rn(q0 - back.x, q1 - back.y));
           }
         }
+      }
       }
       __syncwarp();
 #pragma unroll
@@ -1310,18 +1371,17 @@ constexpr int kJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32) attend_pages_join(const __grid_constant__ AttPagesParams p, int bf_) {
   constexpr int E = D / 32, RF = pg_rec_floats(D);
-  __shared__ float part[kJoinWarps][D], red[kJoinWarps][2];
+  __shared__ float part[kJoinWarps][D], red[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int a = blockIdx.x % p.group, seg = blockIdx.x / p.group;
   const int s = seg / p.pg.heads, h = seg % p.pg.heads;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t total = p.plan[p.items], nc = p.plan[p.items + 1];
-  int64_t t0, t1;
+  const int total = p.plan[p.items], nc = p.plan[p.items + 1], warps = p.plan[p.items + 2];
+  int t0, t1;
   if (p.selected) {
     t0 = p.plan[seg];
     t1 = p.plan[seg + 1];
   } else {
-    const int64_t x = p.plan[s], n = (p.plan[s + 1] - x) / p.pg.heads;
+    const int x = p.plan[s], n = (p.plan[s + 1] - x) / p.pg.heads;
     t0 = x + n * h;
     t1 = t0 + n;
   }
@@ -1332,30 +1392,55 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_pages_join(const __gri
     if (warp == 0) pg_store_out<D>(p, bf_ != 0, s, h, a, lane, y, 0.f);
     return;
   }
-  // CTA c starts at tile floor(total c / nc)
-  const int c0 = (int)(((t0 + 1) * nc - 1) / total), c1 = (int)((t1 * nc - 1) / total);
+  // the CTAs that hold its first and its last tile: the last ones that start at or before them
+  auto cta_of = [&](int t) {
+    int c = min((int)((float)t * ((float)nc / (float)total)), nc - 1);
+    while (c > 0 && pg_start(total, c * warps, nc * warps) > t) --c;
+    while (c + 1 < nc && pg_start(total, (c + 1) * warps, nc * warps) <= t) ++c;
+    return c;
+  };
+  const int c0 = cta_of(t0), c1 = cta_of(t1 - 1);
   if (c0 == c1) return;                            // finished by that CTA
   auto rec = [&](int c) { return p.part + (((int64_t)c * 2 + (c == c0)) * p.group + a) * RF; };
-  float M = -INFINITY;
-  for (int c = c0 + (int)threadIdx.x; c <= c1; c += kJoinWarps * 32) M = fmaxf(M, rec(c)[0]);
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  if (lane == 0) red[warp][0] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, red[w][0]);
+  float M = -INFINITY;                             // of all parts, by every warp
+  for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, rec(c)[0]);
   float l = 0.f;
-#pragma unroll 4
-  for (int c = c0 + warp; c <= c1; c += kJoinWarps) {
-    const float* r = rec(c);
-    const float f = r[0] == -INFINITY ? 0.f : ex2_approx(r[0] - M);
-    l = __fmaf_rn(r[1], f, l);
+  bool first = true;
+  for (int c = c0 + warp; c <= c1; c += 4 * kJoinWarps) {      // four parts at a time
+    float2 ml[4], v[4][E / 2];
 #pragma unroll
-    for (int k = 0; k < E; ++k) y[k] = __fmaf_rn(r[2 + E * lane + k], f, y[k]);
+    for (int i = 0; i < 4; ++i) {
+      const int ci = c + i * kJoinWarps;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (ci <= c1) {
+        const float2* r = reinterpret_cast<const float2*>(rec(ci));
+        ml[i] = r[0];
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) v[i][k] = r[1 + E / 2 * lane + k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) v[i][k] = make_float2(0.f, 0.f);
+      }
+    }
+    if (first) {                                   // while the parts are on their way
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      first = false;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = ml[i].x == -INFINITY ? 0.f : ex2_approx(ml[i].x - M);
+      l = __fmaf_rn(ml[i].y, f, l);
+#pragma unroll
+      for (int k = 0; k < E / 2; ++k) {
+        y[2 * k] = __fmaf_rn(v[i][k].x, f, y[2 * k]);
+        y[2 * k + 1] = __fmaf_rn(v[i][k].y, f, y[2 * k + 1]);
+      }
+    }
   }
 #pragma unroll
   for (int k = 0; k < E; ++k) part[warp][E * lane + k] = y[k];
-  if (lane == 0) red[warp][1] = l;
+  if (lane == 0) red[warp] = l;
   __syncthreads();
   if (warp != 0) return;
   l = 0.f;
@@ -1363,7 +1448,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_pages_join(const __gri
   for (int k = 0; k < E; ++k) y[k] = 0.f;
 #pragma unroll
   for (int w = 0; w < kJoinWarps; ++w) {
-    l += red[w][1];
+    l += red[w];
 #pragma unroll
     for (int k = 0; k < E; ++k) y[k] += part[w][E * lane + k];
   }
@@ -1382,21 +1467,6 @@ static cudaError_t set_smem_once(K kp, std::atomic<int>* ready) {
   return e;
 }
 
-template <int D>
-static cudaError_t launch_join(const AttPagesParams& p, bool bf, cudaStream_t st) {
-  // starts as the main kernel's CTAs leave and waits for its results on the device
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((int64_t)p.pg.seqs * p.pg.heads * p.group));
-  cfg.blockDim = dim3(kJoinWarps * 32);
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_pages_join<D>, p, (int)bf);
-}
-
 template <int D, int QT, bool EXACT>
 static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   using C = Pg<D, QT, EXACT>;
@@ -1411,7 +1481,11 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, tab_v, warp_bytes);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_join<D>(p, !EXACT, st);
+  // an ordinary launch: started while the main kernel runs (programmatic dependent launch) it ended
+  // 3.5 us later in calls of few tokens
+  const unsigned grid = (unsigned)((int64_t)p.pg.seqs * p.pg.heads * p.group);
+  attend_pages_join<D><<<grid, kJoinWarps * 32, 0, st>>>(p, (int)!EXACT);
+  return cudaGetLastError();
 }
 
 // CTAs of the main kernel: one on every SM.

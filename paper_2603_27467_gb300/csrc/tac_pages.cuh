@@ -70,7 +70,7 @@ struct AttPagesParams {
   int64_t q_seq, q_row, o_seq, o_row;      // strides, elements
   int32_t ctas;                            // grid of the main kernel
   int32_t items;                           // spans of tiles: sequences, or (sequence, head)s with `selected`
-  int32_t* plan;                           // workspace: items + 1 first tiles, then the CTAs in use
+  int32_t* plan;                           // workspace: items + 1 first tiles, then the CTAs in use and the warps of each
   float* part;                             // workspace: [ctas][2][group][d + 2]
 };
 

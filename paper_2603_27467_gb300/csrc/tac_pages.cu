@@ -5,14 +5,16 @@
 // power of two.  Minima, maxima and products with powers of two are exact, so the box does
 // not depend on the order of the rows or on how they came (one by one or as a prompt).
 //
-// select_pages: sum_j max(c_j lo_j, c_j hi_j) = sum_j max(c_j, 0) hi_j + min(c_j, 0) lo_j, two
-// dot products of 8-bit numbers a query (dp4a, exact in int32); the powers of two of the
-// query and of the page come last, exact too.  So the order of the scores, and the pages that
+// select_pages: sum_j max(c_j lo_j, c_j hi_j) = sum_j min(c_j, 0) lo_j + max(c_j, 0) hi_j, one dot
+// product of 2 d whole numbers a query (mma.sync on fp16 numbers that hold them, exact); the powers
+// of two of the query and of the page come last, exact too.  (8-bit mma.sync is as exact and runs at
+// 128 products a cycle and SM here: 18.7 us for 8 x 8192 boxes against 13.)  So the order of the scores, and the pages that
 // are chosen, are those of the definition, whatever the kernel's order of summation.
 #include <algorithm>
 #include <atomic>
 
 #include <cooperative_groups.h>
+#include <cuda_fp16.h>
 
 #include "tac_pages.cuh"
 
@@ -256,29 +258,56 @@ cudaError_t launch_page_bounds(int d, int dtype, const BoundsParams& p, int sms,
 // Choice of pages
 // ---------------------------------------------------------------------------
 // A cluster of CTAs takes one (sequence, head): each scores a contiguous part of the pages
-// into shared memory, the largest `budget` are found by radix selection (8 bits a pass,
-// the CTAs' histograms added through distributed shared memory), and every CTA writes its
-// part of them in order.  A score becomes a whole number of the same order.
+// into shared memory.  The threshold, the need-th of the pages in order of (score, lowest index
+// first), is found by one histogram of the scores over equal intervals between the smallest and
+// the largest (the CTAs' counts added through distributed shared memory): the few pages of the
+// interval that holds it are ranked against one another.  Where that interval holds more than
+// kSelList pages (ties, or a few scores far off) the keys are searched by radix selection instead,
+// 8 bits a pass.  Then every CTA writes its part of the choice in order.
+constexpr int kSelBins = 1024;                     // intervals
+constexpr int kSelList = 256;                      // pages ranked against one another
+
+// A score as a whole number of the same order, and back.
 __device__ __forceinline__ uint32_t order_key(float s) {
   const uint32_t u = __float_as_uint(s + 0.f);     // -0 counts as 0
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+constexpr uint32_t kKeyAlways = 0xFFFFFFFFu;       // above every score: a page that is always taken
 
-template <int D, typename T, int NQ>
-__global__ void __launch_bounds__(kPgThreads) select_kernel(const __grid_constant__ SelectParams p) {
-  constexpr int LP = D / 16, PW = 32 / LP;         // lanes a page (16 channels each), pages a warp takes at a time
-  constexpr int R = NQ > LP ? NQ / LP : 1;         // queries a lane holds after the reduction
+// d += a b: one m16n8k16 step, fp16 operands, fp32 sums.
+__device__ __forceinline__ void sel_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kPgThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
+  constexpr int E = D / 32, C = 2 * D / 64;        // C: 16-byte pieces of a box a lane takes (4 lanes a box)
   extern __shared__ uint32_t keys[];               // of this CTA's pages
-  __shared__ __align__(16) int qpos[NQ][D / 4], qneg[NQ][D / 4];
-  __shared__ float qscale[NQ];
-  __shared__ uint32_t hist[4][256];                // one for each pass: a CTA may lag behind a pass
+  __shared__ __align__(16) uint32_t qfrag[C][2][32][4];   // [piece][half of it][lane]: a query's codes as halves
+  __shared__ float qscale[8], qbias[8];            // the power of two; 128 times the sum of the codes
+  __shared__ __align__(16) uint32_t hist[kSelBins];   // counts of an interval (radix: of four passes, 256 each)
+  __shared__ uint2 list[kSelList], whole[kSelList];   // (key, page) in the threshold's interval: this CTA's, the cluster's
+  __shared__ __align__(8) int mine[2];                        // how many there are in list; pages above the interval here
   __shared__ uint32_t range[2];                    // smallest and largest key here
-  __shared__ int counts[2];                        // pages above the threshold, at it
-  __shared__ int wsum[kPgWarps][2], scan[kPgWarps + 1], found[2];
+  __shared__ int counts[2];                        // pages of the threshold's key here (radix), pages taken here
+  __shared__ uint2 cut;                            // the last (key, page) that is taken (radix: of the first CTA)
+  __shared__ int wsum[kPgWarps], scan[kPgWarps + 1], found[3];
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  auto sync = [&]() { if (cs == 1) __syncthreads(); else cluster.sync(); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int seg = blockIdx.x / cs, s = seg / p.pg.heads, h = seg % p.pg.heads;
+  static_assert(kPgWarps == 8, "a warp a query");
+  float x[E];                                      // query `warp`: asked for first
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    x[e] = 0.f;
+    if (warp < p.group)
+      x[e] = to_f<T>(reinterpret_cast<const T*>(p.q)[(int64_t)s * p.seq_stride + ((int64_t)h * p.group + warp) * p.row_stride + lane * E + e]);
+  }
   const int64_t len = min((int64_t)max(p.pg.lengths[s], 0), (int64_t)p.pg.width * p.pg.page);
   const int n = (int)((len + p.pg.page - 1) / p.pg.page);
   const int chunk = (n + cs - 1) / cs, first = min(rank * chunk, n), cnt = min(n - first, chunk);
@@ -292,17 +321,46 @@ __global__ void __launch_bounds__(kPgThreads) select_kernel(const __grid_constan
     for (int i = tid; i < cnt; i += kPgThreads) out[first + i] = first + i;
     return;
   }
+  // This warp's pages: a contiguous part, in tiles of 16.  Rows of an mma are pages: lane (g, t)
+  // takes pieces t, t + 4, ... of the boxes of pages g and g + 8, as they lie in memory; the
+  // queries' codes are arranged to match.  Table entries and scales of 128 pages are loaded at
+  // once, a tile's boxes while the one before it is scored.
+  const int g = lane >> 2, t = lane & 3;
+  const int per = (cnt + kPgWarps - 1) / kPgWarps;
+  const int w_lo = min(warp * per, cnt), w_hi = min(w_lo + per, cnt);
+  const int32_t* row = p.pg.table + (int64_t)s * p.pg.table_stride + first;
+  constexpr int WIN = 4;                           // a lane's pages of a window: lane, lane + 32, ...
+  int ph[WIN];
+  float sp[WIN];
+  auto window = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < WIN; ++i) ph[i] = base + 32 * i + lane < w_hi ? row[base + 32 * i + lane] : -1;
+#pragma unroll
+    for (int i = 0; i < WIN; ++i) {
+      if (ph[i] >= p.pg.pages) ph[i] = -1;
+      sp[i] = ph[i] >= 0 ? p.scales[(int64_t)ph[i] * p.pg.heads + h] : 0.f;
+    }
+  };
+  auto pick = [&](auto (&v)[WIN], int tile) { return tile < 4 ? (tile < 2 ? v[0] : v[1]) : (tile < 6 ? v[2] : v[3]); };
+  auto ask = [&](int tile, uint4 (&box)[2][C]) {   // tile of the window
+    const int mine_ = pick(ph, tile);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int e = __shfl_sync(0xffffffffu, mine_, 16 * (tile & 1) + g + 8 * r);
+      const uint4* b = reinterpret_cast<const uint4*>(p.codes + ((int64_t)max(e, 0) * p.pg.heads + h) * 2 * D) + t;
+#pragma unroll
+      for (int j = 0; j < C; ++j) box[r][j] = e >= 0 ? b[4 * j] : make_uint4(0, 0, 0, 0);
+    }
+  };
+  uint4 box[2][C];
+  window(w_lo);
+  ask(0, box);
 
-  // ---- the queries in 8 bits, positive and negative parts apart ----
-  if (warp < NQ) {
-    constexpr int E = D / 32;
-    float x[E];
+  // ---- the queries in 8 bits ----
+  {
     float a = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      x[e] = 0.f;
-      if (warp < p.group)
-        x[e] = to_f<T>(reinterpret_cast<const T*>(p.q)[(int64_t)s * p.seq_stride + ((int64_t)h * p.group + warp) * p.row_stride + lane * E + e]);
       if (!(fabsf(x[e]) < INFINITY)) x[e] = 0.f;
       a = fmaxf(a, fabsf(x[e]));
     }
@@ -310,109 +368,77 @@ __global__ void __launch_bounds__(kPgThreads) select_kernel(const __grid_constan
     for (int o = 16; o >= 1; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
     const int ex = box_exp(a);
     const float inv = pow2i(-ex);
-    int pos = 0, neg = 0;
+    // byte z of a box (lo, then hi) meets the code's negative part below D, its positive part from D on;
+    // it is byte z % 16 of piece z / 16, which lane t = (z / 16) % 4 of a page takes
+    int sum = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = __float2int_rn(x[e] * inv);
-      pos |= (max(c, 0) & 0xFF) << (8 * e);
-      neg |= (min(c, 0) & 0xFF) << (8 * e);
+      sum += c;
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        const int z = side * D + lane * E + e, piece = z / 16, word = z % 16 / 4;
+        __half* const at = reinterpret_cast<__half*>(&qfrag[piece / 4][word / 2][4 * warp + piece % 4][2 * (word % 2)]);
+        at[z % 4] = __int2half_rn(side ? max(c, 0) : min(c, 0));
+      }
     }
-    if constexpr (E == 4) {
-      qpos[warp][lane] = pos;
-      qneg[warp][lane] = neg;
-    } else {
-      reinterpret_cast<uint16_t*>(qpos[warp])[lane] = (uint16_t)pos;
-      reinterpret_cast<uint16_t*>(qneg[warp])[lane] = (uint16_t)neg;
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    if (lane == 0) {
+      qscale[warp] = pow2i(ex);
+      qbias[warp] = 128.f * (float)sum;
     }
-    if (lane == 0) qscale[warp] = pow2i(ex);
   }
-  for (int i = tid; i < 4 * 256; i += kPgThreads) hist[0][i] = 0u;
-  if (tid == 0) { range[0] = 0xFFFFFFFFu; range[1] = 0u; }
+  for (int i = tid; i < kSelBins; i += kPgThreads) hist[i] = 0u;
+  if (tid == 0) { range[0] = 0xFFFFFFFFu; range[1] = 0u; mine[0] = mine[1] = 0; }
   __syncthreads();
 
   // ---- scores ----
   {
-    const int sub = lane % LP, g = lane / LP;
-    int qp[NQ][4], qn[NQ][4];
-#pragma unroll
-    for (int a = 0; a < NQ; ++a) {
-      const int4 x = *reinterpret_cast<const int4*>(&qpos[a][4 * sub]), y = *reinterpret_cast<const int4*>(&qneg[a][4 * sub]);
-      qp[a][0] = x.x; qp[a][1] = x.y; qp[a][2] = x.z; qp[a][3] = x.w;
-      qn[a][0] = y.x; qn[a][1] = y.y; qn[a][2] = y.z; qn[a][3] = y.w;
-    }
-    // after the reduction over a page's lanes this one holds R queries from q0 on
-    int q0 = 0;
-    {
-      int c = NQ;
-#pragma unroll
-      for (int o = LP / 2; o >= 1; o >>= 1)
-        if (c > 1) { c /= 2; q0 += sub & o ? c : 0; }
-    }
-    float qs[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) qs[i] = qscale[q0 + i];
+    // A box's bytes plus 128 are the halves (c + 128) 2^-24 (subnormal: the bits are the number), and
+    // the sums, whole multiples of 2^-24 below 2^22 of them, are exact; 128 times the codes' sum
+    // comes off afterwards.
+    const float qs0 = qscale[2 * t], qs1 = qscale[2 * t + 1], qb0 = qbias[2 * t], qb1 = qbias[2 * t + 1];
+    const bool in0 = 2 * t < p.group, in1 = 2 * t + 1 < p.group;
     uint32_t kmin = 0xFFFFFFFFu, kmax = 0u;
-    const int32_t* row = p.pg.table + (int64_t)s * p.pg.table_stride + first;
-    for (int base = warp * 32; base < cnt; base += kPgThreads) {
-      int64_t at = -1;                             // box of page base + lane
-      float sp = 0.f;
-      if (base + lane < cnt) {
-        const int ph = row[base + lane];
-        if (ph >= 0 && ph < p.pg.pages) {
-          at = (int64_t)ph * p.pg.heads + h;
-          sp = p.scales[at];
+#pragma unroll 1
+    for (int base = w_lo, tile = 0; base < w_hi; base += 16, ++tile) {
+      if (tile == 2 * WIN) {                       // the next window
+        tile = 0;
+        window(base);
+        ask(0, box);
+      }
+      uint4 next[2][C];
+      if (tile + 1 < 2 * WIN && base + 16 < w_hi) ask(tile + 1, next);
+      float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        const uint32_t u[4] = {box[0][j].x ^ 0x80808080u, box[0][j].y ^ 0x80808080u, box[0][j].z ^ 0x80808080u, box[0][j].w ^ 0x80808080u};
+        const uint32_t v[4] = {box[1][j].x ^ 0x80808080u, box[1][j].y ^ 0x80808080u, box[1][j].z ^ 0x80808080u, box[1][j].w ^ 0x80808080u};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint2 q = *reinterpret_cast<const uint2*>(&qfrag[j][k / 2][lane][2 * (k % 2)]);
+          sel_mma(d, __byte_perm(u[k], 0u, 0x4140), __byte_perm(v[k], 0u, 0x4140), __byte_perm(u[k], 0u, 0x4342),
+                  __byte_perm(v[k], 0u, 0x4342), q.x, q.y);
         }
       }
-#pragma unroll 4
-      for (int it = 0; it < LP; ++it) {
-        const int64_t box = __shfl_sync(0xffffffffu, at, it * PW + g);
-        const float f = __shfl_sync(0xffffffffu, sp, it * PW + g);
-        int4 lo = make_int4(0, 0, 0, 0), hi = lo;
-        if (box >= 0) {
-          const int4* b = reinterpret_cast<const int4*>(p.codes + box * 2 * D) + sub;
-          lo = b[0];
-          hi = b[D / 16];
-        }
-        int v[NQ];
 #pragma unroll
-        for (int a = 0; a < NQ; ++a) {
-          int x = __dp4a(qp[a][0], hi.x, 0);
-          x = __dp4a(qn[a][0], lo.x, x);
-          x = __dp4a(qp[a][1], hi.y, x);
-          x = __dp4a(qn[a][1], lo.y, x);
-          x = __dp4a(qp[a][2], hi.z, x);
-          x = __dp4a(qn[a][2], lo.z, x);
-          x = __dp4a(qp[a][3], hi.w, x);
-          v[a] = __dp4a(qn[a][3], lo.w, x);
-        }
-        int c = NQ;
-#pragma unroll
-        for (int o = LP / 2; o >= 1; o >>= 1) {
-          if (c > 1) {
-            c /= 2;
-            const bool up = sub & o;
-#pragma unroll
-            for (int i = 0; i < c; ++i) {
-              const int give = up ? v[i] : v[i + c], keep = up ? v[i + c] : v[i];
-              v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-            }
-          } else {
-            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-          }
-        }
-        float best = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-          if (q0 + i < p.group) best = fmaxf(best, fmaxf(fminf(((float)v[i] * qs[i]) * f, kFltMax), -kFltMax));
-#pragma unroll
-        for (int o = LP / 2; o >= 1; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-        if (box < 0) best = -INFINITY;
+      for (int r = 0; r < 2; ++r) {                // page base + 8 r + g, queries 2 t and 2 t + 1
+        const bool have = __shfl_sync(0xffffffffu, pick(ph, tile), 16 * (tile & 1) + g + 8 * r) >= 0;
+        const float f = __shfl_sync(0xffffffffu, pick(sp, tile), 16 * (tile & 1) + g + 8 * r);
+        auto score = [&](float v, float qs, float bias) {
+          return fmaxf(fminf((__fmaf_rn(v, 16777216.f, -bias) * qs) * f, kFltMax), -kFltMax);
+        };
+        float best = in0 ? score(d[2 * r], qs0, qb0) : -INFINITY;
+        if (in1) best = fmaxf(best, score(d[2 * r + 1], qs1, qb1));
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+        if (!have) best = -INFINITY;
         else if (f == INFINITY) best = kFltMax;
-        const int i = base + it * PW + g, page = first + i;
-        if (sub == 0 && i < cnt) {
+        const int i = base + 8 * r + g, page = first + i;
+        if (t == 0 && i < w_hi) {
           uint32_t key = order_key(best);
           if (page < p.keep_first || page >= n - p.keep_last) {
-            key = 0xFFFFFFFFu;                     // above every score: always taken
+            key = kKeyAlways;
           } else {
             kmin = min(kmin, key);
             kmax = max(kmax, key);
@@ -420,6 +446,10 @@ __global__ void __launch_bounds__(kPgThreads) select_kernel(const __grid_constan
           keys[i] = key;
         }
       }
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < C; ++j) box[r][j] = next[r][j];
     }
     kmin = __reduce_min_sync(0xffffffffu, kmin);
     kmax = __reduce_max_sync(0xffffffffu, kmax);
@@ -428,86 +458,180 @@ __global__ void __launch_bounds__(kPgThreads) select_kernel(const __grid_constan
       atomicMax(&range[1], kmax);
     }
   }
-  cluster.sync();
+  sync();
 
-  // ---- the threshold: the need-th largest of the keys that are not always taken ----
+  // ---- the cut: pages of larger keys, and of its key up to its index, are taken ----
   int need = p.budget - p.keep_first - p.keep_last;
-  uint32_t thr = 0xFFFFFFFFu;
+  uint2 last = make_uint2(kKeyAlways, 0u);         // only those that are always taken
+  bool counted = false;                            // before_me is known: pages taken by the CTAs before
+  int before_me = 0;
   if (need > 0) {
     uint32_t kmin = 0xFFFFFFFFu, kmax = 0u;
-    for (int r = 0; r < cs; ++r) {
-      const uint32_t* x = cluster.map_shared_rank(range, r);
-      kmin = min(kmin, x[0]);
-      kmax = max(kmax, x[1]);
+    if (lane < cs) {
+      const uint32_t* x = cluster.map_shared_rank(range, lane);
+      kmin = x[0];
+      kmax = x[1];
     }
-    // the bits above the first that differs are common to all
-    int low = kmin == kmax ? 0 : 32 - __clz(kmin ^ kmax);
-    uint32_t fixed = low == 32 ? 0u : kmax >> low << low;
-    for (int pass = 0; low > 0; ++pass) {
-      const int bits = min(low, 8), at = low - bits;
-      const uint32_t above = low == 32 ? 0u : 0xFFFFFFFFu << low;
-      for (int i = tid; i < cnt; i += kPgThreads) {
-        const uint32_t k = keys[i];
-        if (k != 0xFFFFFFFFu && (k & above) == fixed) atomicAdd(&hist[pass][(k >> at) & 255u & ((1u << bits) - 1u)], 1u);
+    kmin = __reduce_min_sync(0xffffffffu, kmin);
+    kmax = __reduce_max_sync(0xffffffffu, kmax);
+    if (kmin == kmax) {                            // all alike: the first `need` in order
+      last.x = kmin;
+      last.y = (uint32_t)(p.keep_first + need - 1);
+    } else {
+      // intervals of equal width; a score's interval does not fall as the score rises
+      const float s_lo = key_score(kmin), width = (float)kSelBins / (key_score(kmax) - s_lo);
+      bool radix = !(width > 0.f && width < INFINITY && s_lo > -INFINITY);
+      auto bin_of = [&](uint32_t k) { return min(max((int)((key_score(k) - s_lo) * width), 0), kSelBins - 1); };
+      int bin = 0;
+      if (!radix) {
+        for (int i = tid; i < cnt; i += kPgThreads)
+          if (keys[i] != kKeyAlways) atomicAdd(&hist[bin_of(keys[i])], 1u);
+        sync();
+        // this thread: the four intervals below kSelBins - 4 tid
+        constexpr int B = kSelBins / kPgThreads;
+        static_assert(B == 4, "a thread's intervals are one 16-byte word");
+        int c[B] = {};
+#pragma unroll 4
+        for (int r = 0; r < cs; ++r) {
+          const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist, r) + kSelBins - B * (tid + 1));
+          c[0] += (int)x.w; c[1] += (int)x.z; c[2] += (int)x.y; c[3] += (int)x.x;
+        }
+        int total;
+        int before = block_prefix(c[0] + c[1] + c[2] + c[3], scan, &total);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          if (before < need && need <= before + c[i]) {
+            found[0] = kSelBins - 1 - (B * tid + i);
+            found[1] = need - before;
+            found[2] = c[i];
+          }
+          before += c[i];
+        }
+        __syncthreads();
+        bin = found[0];
+        radix = found[2] > kSelList;               // the same for every CTA of the cluster
+        if (!radix) {
+          const int rest = found[1], m = found[2];
+          int up = 0;                              // pages above the interval (and those always taken)
+          for (int i = tid; i < cnt; i += kPgThreads) {
+            const uint32_t k = keys[i];
+            const int kb = k == kKeyAlways ? kSelBins : bin_of(k);
+            up += kb > bin;
+            if (kb == bin) list[atomicAdd(&mine[0], 1)] = make_uint2(k, (uint32_t)(first + i));
+          }
+          up = __reduce_add_sync(0xffffffffu, up);
+          if (lane == 0) atomicAdd(&mine[1], up);
+          sync();
+          // every CTA takes all lists, in the order of the CTAs, and ranks their pages
+          int2 c2 = make_int2(0, 0);
+          if (lane < cs) c2 = *reinterpret_cast<const int2*>(cluster.map_shared_rank(mine, lane));
+          int off = 0, mylist = 0;
+          for (int r = 0; r < cs; ++r) {
+            const int nl = __shfl_sync(0xffffffffu, c2.x, r), nu = __shfl_sync(0xffffffffu, c2.y, r);
+            if (tid >= off && tid < off + nl) whole[tid] = cluster.map_shared_rank(list, r)[tid - off];
+            if (r == rank) mylist = off;
+            if (r < rank) before_me += nu;
+            off += nl;
+          }
+          __syncthreads();
+          bool in = false;
+          if (tid < m) {
+            const uint2 me = whole[tid];
+            int above = 0;
+#pragma unroll 4
+            for (int j = 0; j < m; ++j) {
+              const uint2 o = whole[j];
+              above += o.x > me.x || (o.x == me.x && o.y < me.y);
+            }
+            in = above < rest;
+            if (above == rest - 1) cut = me;
+          }
+          before_me += __syncthreads_count(in && tid < mylist);
+          last = cut;
+          counted = true;
+        }
       }
-      cluster.sync();
-      // digit 255 - tid: how many keys have a larger one
-      int c = 0;
-      for (int r = 0; r < cs; ++r) c += (int)cluster.map_shared_rank(hist[pass], r)[255 - tid];
-      int total;
-      const int before = block_prefix(c, scan, &total);
-      if (before < need && need <= before + c) { found[0] = 255 - tid; found[1] = need - before; }
-      __syncthreads();
-      fixed |= (uint32_t)found[0] << at;
-      need = found[1];
-      low = at;
+      if (radix) {
+        sync();                                    // the histograms are read
+        for (int i = tid; i < kSelBins; i += kPgThreads) hist[i] = 0u;
+        sync();
+        // the bits above the first that differs are common to all
+        int low = 32 - __clz(kmin ^ kmax);
+        uint32_t fixed = low == 32 ? 0u : kmax >> low << low;
+        for (int pass = 0; low > 0; ++pass) {
+          const int bits = min(low, 8), at = low - bits;
+          const uint32_t above = low == 32 ? 0u : 0xFFFFFFFFu << low;
+          for (int i = tid; i < cnt; i += kPgThreads) {
+            const uint32_t k = keys[i];
+            if (k != kKeyAlways && (k & above) == fixed) atomicAdd(&hist[256 * pass + ((k >> at) & ((1u << bits) - 1u))], 1u);
+          }
+          sync();
+          int c = 0;                               // digit 255 - tid
+          for (int r = 0; r < cs; ++r) c += (int)cluster.map_shared_rank(hist, r)[256 * pass + 255 - tid];
+          int total;
+          const int before = block_prefix(c, scan, &total);
+          if (before < need && need <= before + c) { found[0] = 255 - tid; found[1] = need - before; }
+          __syncthreads();
+          fixed |= (uint32_t)found[0] << at;
+          need = found[1];
+          low = at;
+        }
+        // the need-th page of that key, in order
+        int eq = 0;
+        for (int i = w_lo + lane; i < w_hi; i += 32) eq += keys[i] == fixed;
+        eq = __reduce_add_sync(0xffffffffu, eq);
+        if (lane == 0) wsum[warp] = eq;
+        __syncthreads();
+        int all = 0;
+        for (int w = 0; w < kPgWarps; ++w) {
+          if (w == warp) eq = all;
+          all += wsum[w];
+        }
+        if (tid == 0) counts[0] = all;
+        sync();
+        for (int r = 0; r < rank; ++r) eq += cluster.map_shared_rank(counts, r)[0];
+        for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
+          const bool e = i0 + lane < w_hi && keys[i0 + lane] == fixed;
+          const uint32_t m = __ballot_sync(0xffffffffu, e);
+          if (e && eq + __popc(m & ((1u << lane) - 1u)) == need - 1) *cluster.map_shared_rank(&cut, 0) = make_uint2(fixed, (uint32_t)(first + i0 + lane));
+          eq += __popc(m);
+        }
+        sync();
+        last = *cluster.map_shared_rank(&cut, 0);
+      }
     }
-    thr = fixed;
   }
 
-  // ---- the pages above the threshold and the first `need` at it, in order ----
-  const int per = (cnt + kPgThreads - 1) / kPgThreads * 32, lo = min(warp * per, cnt), hi = min(lo + per, cnt);
-  int gt = 0, eq = 0;
-  for (int i = lo + lane; i < hi; i += 32) {
-    const uint32_t k = keys[i];
-    const bool e = k == thr && thr != 0xFFFFFFFFu;
-    gt += !e && k >= thr;
-    eq += e;
-  }
-  gt = __reduce_add_sync(0xffffffffu, gt);
-  eq = __reduce_add_sync(0xffffffffu, eq);
-  if (lane == 0) { wsum[warp][0] = gt; wsum[warp][1] = eq; }
+  // ---- the pages up to the cut, in order ----
+  auto taken = [&](int i) { const uint32_t k = keys[i]; return k > last.x || (k == last.x && (uint32_t)(first + i) <= last.y) || k == kKeyAlways; };
+  int c = 0;
+  for (int i = w_lo + lane; i < w_hi; i += 32) c += taken(i);
+  c = __reduce_add_sync(0xffffffffu, c);
+  if (lane == 0) wsum[warp] = c;
   __syncthreads();
-  if (tid == 0) {
-    int a = 0, b = 0;
-    for (int w = 0; w < kPgWarps; ++w) { a += wsum[w][0]; b += wsum[w][1]; }
-    counts[0] = a;
-    counts[1] = b;
+  int all = 0, at = 0;
+  for (int w = 0; w < kPgWarps; ++w) {
+    if (w == warp) at = all;
+    all += wsum[w];
   }
-  cluster.sync();
-  gt = eq = 0;                                     // before this warp's pages
-  for (int r = 0; r < rank; ++r) {
-    const int* x = cluster.map_shared_rank(counts, r);
-    gt += x[0];
-    eq += x[1];
+  if (cs > 1 && !counted) {
+    if (tid == 0) counts[1] = all;
+    sync();
+    for (int r = 0; r < rank; ++r) before_me += cluster.map_shared_rank(counts, r)[1];
   }
-  for (int w = 0; w < warp; ++w) { gt += wsum[w][0]; eq += wsum[w][1]; }
-  for (int i0 = lo; i0 < hi; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t k = i < hi ? keys[i] : 0u;
-    const bool e = i < hi && k == thr && thr != 0xFFFFFFFFu, a = i < hi && !e && k >= thr;
-    const uint32_t am = __ballot_sync(0xffffffffu, a), em = __ballot_sync(0xffffffffu, e), below = (1u << lane) - 1u;
-    const int mg = gt + __popc(am & below), me = eq + __popc(em & below);
-    if (a || (e && me < need)) out[mg + min(me, need)] = first + i;
-    gt += __popc(am);
-    eq += __popc(em);
+  at += before_me;
+  for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
+    const bool t = i0 + lane < w_hi && taken(i0 + lane);
+    const uint32_t m = __ballot_sync(0xffffffffu, t);
+    if (t) out[at + __popc(m & ((1u << lane) - 1u))] = first + i0 + lane;
+    at += __popc(m);
   }
-  cluster.sync();                                  // the others may still read this CTA's counts
+  if (cs > 1) sync();                              // the others may still read this CTA's memory
 }
 
-template <int D, typename T, int NQ>
+template <int D, typename T>
 static cudaError_t launch_select_t(const SelectParams& p, int sms, cudaStream_t st) {
-  auto kp = select_kernel<D, T, NQ>;
+  auto kp = select_kernel<D, T>;
   static std::atomic<int> ready[64];               // per device: the shared-memory limit is set
   int dev = 0;
   cudaGetDevice(&dev);
@@ -520,7 +644,7 @@ static cudaError_t launch_select_t(const SelectParams& p, int sms, cudaStream_t 
   const int64_t segs = (int64_t)p.pg.seqs * p.pg.heads;
   if (segs < 1) return cudaSuccess;
   int cs = 1;
-  while (cs < 8 && (segs * cs < 2 * sms || p.pg.width > cs * 32768) && p.pg.width > cs * 64) cs *= 2;
+  while (cs < 8 && (segs * cs * 2 <= sms || p.pg.width > cs * 32768) && p.pg.width > cs * 128) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(segs * cs));
   cfg.blockDim = dim3(kPgThreads);
@@ -536,10 +660,8 @@ static cudaError_t launch_select_t(const SelectParams& p, int sms, cudaStream_t 
 }
 
 cudaError_t launch_select_pages(int d, int dtype, const SelectParams& p, int sms, cudaStream_t st) {
-#define TAC_SEL(DD, T) (p.group <= 4 ? launch_select_t<DD, T, 4>(p, sms, st) : launch_select_t<DD, T, 8>(p, sms, st))
-  if (dtype == TAC_BF16) return d == 128 ? TAC_SEL(128, __nv_bfloat16) : TAC_SEL(64, __nv_bfloat16);
-  return d == 128 ? TAC_SEL(128, float) : TAC_SEL(64, float);
-#undef TAC_SEL
+  if (dtype == TAC_BF16) return d == 128 ? launch_select_t<128, __nv_bfloat16>(p, sms, st) : launch_select_t<64, __nv_bfloat16>(p, sms, st);
+  return d == 128 ? launch_select_t<128, float>(p, sms, st) : launch_select_t<64, float>(p, sms, st);
 }
 
 }  // namespace tac

@@ -215,10 +215,13 @@ struct Cursor {
 // A batch: two tiles (the second may be missing) of one (sequence, head).
 struct Batch {
   uint32_t t0, t1;       // first record slots / 16
-  int valid0, valid1;    // tokens of each tile that count (0: nothing is copied)
-  int seq, head;
-  bool begins, first;    // the warp's first batch of this (sequence, head); which starts with tile 0
+  uint32_t valid;        // tokens of each tile that count (16 bits each; 0: nothing is copied)
+  bool first;            // it starts with tile 0 of the (sequence, head)
   bool ends, last;       // the warp's last batch of it; which holds its last tile
+  __device__ __forceinline__ int valid0() const { return (int)(valid & 0xFFFFu); }
+  __device__ __forceinline__ int valid1() const { return (int)(valid >> 16); }
+  __device__ __forceinline__ bool half(int hf) const { return hf ? valid >> 16 : valid & 0xFFFFu; }
+  __device__ __forceinline__ bool full() const { return valid == (kTile << 16 | kTile); }
 };
 
 // Where tile i of the cursor's (sequence, head) is, and how many of its tokens count.
@@ -272,11 +275,7 @@ __device__ __forceinline__ bool cursor_next(const AttPagesParams& p, Cursor& c, 
   }
   b.t0 = __shfl_sync(0xffffffffu, c.t0, c.j);
   b.t1 = __shfl_sync(0xffffffffu, c.t1, c.j);
-  const uint32_t v = __shfl_sync(0xffffffffu, c.valid, c.j);
-  b.valid0 = (int)(v & 0xFFFFu);
-  b.valid1 = (int)(v >> 16);
-  b.seq = c.seq;
-  b.head = c.head;
+  b.valid = __shfl_sync(0xffffffffu, c.valid, c.j);
   b.first = c.first && c.j == 0;
   ++c.j;
   b.ends = c.done && c.j == c.n;
@@ -585,10 +584,11 @@ __device__ __forceinline__ uint32_t pg_log_norm(uint32_t w, int j, uint32_t sl) 
 // what rounding the two moved the largest code by.
 __device__ __forceinline__ uint32_t pg_log_consts(float2 h, int nc, float& factor) {
   const bool spread = h.y > h.x;
-  const float d = spread ? (lg2_approx(h.y) - lg2_approx(h.x)) * (nc == 3 ? 1.f / 255.f : 1.f / 15.f) : 0.f;
+  constexpr float kUp = 1099511627776.f;           // 2^40: subnormal norms become normal numbers
+  const float d = spread ? (lg2_ftz(h.y * kUp) - lg2_ftz(h.x * kUp)) * (nc == 3 ? 1.f / 255.f : 1.f / 15.f) : 0.f;
   const __half slope = __float2half_rn(d), off = nc == 3 ? __float2half_rn(0.f) : __float2half_rn(-31.f * __half2float(slope));
   const float moved = nc == 3 ? 0.f : __fmaf_rn(31.f, __half2float(slope), __half2float(off));
-  factor = h.y * ex2_approx(-moved);
+  factor = h.y * ex2_ftz(-moved);
   return h2_bits(__halves2half2(slope, off));
 }
 
@@ -646,22 +646,22 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   };
   const uint32_t stage_k = pg_smem(st_k), stage_v = pg_smem(st_v);
   auto issue = [&](const Book& bk, uint32_t stage, uint32_t bar, const Batch& b) {
-    if (dead || (b.valid0 | b.valid1) == 0) return;
+    if (dead || b.valid == 0) return;
     if (pg_elect()) {
       const int tile = kTile * (bk.ab + bk.nb + bk.hb);
-      if (b.valid0 && b.valid1 && b.t1 == b.t0 + 1) {
+      if (b.half(0) && b.half(1) && b.t1 == b.t0 + 1) {
         pg_bar_expect(bar, 2 * tile);
         copy_rows(bk, stage, bar, b.t0, 0, kBatch);
       } else {
-        pg_bar_expect(bar, ((b.valid0 > 0) + (b.valid1 > 0)) * tile);
-        if (b.valid0) copy_rows(bk, stage, bar, b.t0, 0, kTile);
-        if (b.valid1) copy_rows(bk, stage, bar, b.t1, 1, kTile);
+        pg_bar_expect(bar, (b.half(0) + b.half(1)) * tile);
+        if (b.half(0)) copy_rows(bk, stage, bar, b.t0, 0, kTile);
+        if (b.half(1)) copy_rows(bk, stage, bar, b.t1, 1, kTile);
       }
     }
     __syncwarp();
   };
   auto landed = [&](const Batch& b, uint32_t bar, uint32_t& phase) {
-    if ((b.valid0 | b.valid1) != 0 && !dead) {
+    if (b.valid != 0 && !dead) {
       dead = !__all_sync(0xffffffffu, pg_bar_wait(bar, phase));
       phase ^= 1u;
     }
@@ -669,8 +669,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   };
   Batch b, nx;
   bool more = cursor_next(p, cur, lane, nx);
+  bool begins = true;                              // the next batch is the first of its (sequence, head)
+  int seq = 0, head = 0;                           // the (sequence, head) at hand
   if (more) {
-    nx.begins = true;
     issue(p.k, stage_k, bar_k, nx);
     issue(p.v, stage_v, bar_v, nx);
   }
@@ -715,7 +716,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
       for (int x = 0; x < QT; ++x) { sv[x][0] = sv[x][2]; sv[x][1] = sv[x][3]; }
-      if ((hf ? b.valid1 : b.valid0) == 0) continue;
+      if (!b.half(hf)) continue;
       float2 s[NQ][2];
 #pragma unroll
       for (int a = 0; a < NQ; ++a) s[a][0] = s[a][1] = make_float2(0.f, 0.f);
@@ -850,7 +851,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     for (int hf = 0; hf < 2; ++hf, arow += kTile * kab, nrow += kTile * knb, cst += kTile) {
 #pragma unroll
       for (int x = 0; x < QT; ++x) { sv[x][0] = sv[x][2]; sv[x][1] = sv[x][3]; }
-      if ((hf ? b.valid1 : b.valid0) == 0) continue;
+      if (!b.half(hf)) continue;
       Run<W, KP> run[2];
       uint32_t nw[2][KW], sl[2];
       float2 ab[2];
@@ -922,10 +923,12 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 
   // Rows of the values' fragments are positions, steps run over (token, cos | sin); column 2 a + c has
   // query a's weights in the rows of component c and zeros in the others, so that a looked-up
-  // (cos, sin) goes in as it is.  w1, w2: the weights of this lane's tokens g, g + 8 of a tile (query
-  // 4 x + t) as two halves; they are handed to the lanes that need them by shuffles.
+  // (cos, sin) goes in as it is.  A weight is 2^(s - m) times V's factor of the token, over a power of
+  // two that keeps the largest so far below 2^14, as a half; it is worked out where its score is
+  // (token g or g + 8 of a tile, query 4 x + t) and handed on by shuffles.  fix: what the sums so
+  // far are multiplied by because the maximum moved.
   const uint32_t put0 = g & 1 ? 0x1044u : 0x4410u, put1 = g & 1 ? 0x3244u : 0x4432u;
-  auto values_mma = [&](const uint32_t (&w1)[QT][2], const uint32_t (&w2)[QT][2], auto nc_, auto w_) {
+  auto values_mma = [&](const float (&pr)[QT][4], const float (&fix)[QT], bool m_moved, auto nc_, auto w_) {
     constexpr int NC = decltype(nc_)::value, W = decltype(w_)::value;
     constexpr bool F32N = NC == 4, LIN = NC == 0 || NC == 2;
     constexpr int VB = NC <= 1 ? 4 : 8;
@@ -936,9 +939,38 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
     const uint8_t* arow = st_v + t * vab + (vbit >> 5) * 4;
     const uint8_t* nrow = st_vn + t * vnb + (F32N ? 4 * VP * g : VP * VB * g / 8);
     const uint32_t* cst = vd + t;
+    uint32_t w1[QT][2], w2[QT][2];
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      float wa[4], wb[4], wm = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2* f = vc + 16 * (i >> 1) + 8 * (i & 1) + g;
+        wb[i] = pr[x][i] * f->y;
+        wa[i] = LIN ? pr[x][i] * f->x : 0.f;
+        wm = LIN ? max3(wm, wa[i], wb[i]) : fmaxf(wm, wb[i]);
+      }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+      const int ex = max(ae[x], min(pg_exp_of(wm) - 13, 126)), by = ae[x] - ex;
+      if (__any_sync(0xffffffffu, m_moved || by != 0)) {
+        const float f = fix[x] * (by < -252 ? 0.f : pg_exp2i(by / 2) * pg_exp2i(by - by / 2));
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) am[x][m][i] *= f;
+      }
+      ae[x] = ex;
+      const float sc = pow2i(-ex);                 // -126 <= ex <= 126
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        w1[x][i] = LIN ? h2_bits(__floats2half2_rn(wa[2 * i] * sc, wa[2 * i + 1] * sc)) : 0u;
+        w2[x][i] = h2_bits(__floats2half2_rn(wb[2 * i] * sc, wb[2 * i + 1] * sc));
+      }
+    }
 #pragma unroll 1
     for (int hf = 0; hf < 2; ++hf, arow += kTile * vab, nrow += kTile * vnb, cst += kTile) {
-      if ((hf ? b.valid1 : b.valid0) == 0) continue;
+      if (!b.half(hf)) continue;
       uint32_t p1[QT][2], p2[QT][2];               // tokens t, t + 8 | t + 4, t + 12 of query g / 2
 #pragma unroll
       for (int x = 0; x < QT; ++x)
@@ -1044,8 +1076,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 
   while (more) {
     b = nx;
-    if (b.begins) {                                // a new (sequence, head)
+    if (begins) {                                  // a new (sequence, head): still the cursor's
       begun = b.first;
+      seq = cur.seq;
+      head = cur.head;
       __syncwarp();
 #pragma unroll 1
       for (int a0 = 0; a0 < NQ; a0 += 4) {
@@ -1054,7 +1088,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
       for (int a = 0; a < 4; ++a) {
 #pragma unroll
         for (int k = 0; k < E; ++k) yy[a][k] = 0.f;
-        if (a0 + a < p.group) pg_load_query<D>(p, bf, b.seq, b.head, a0 + a, lane, yy[a]);
+        if (a0 + a < p.group) pg_load_query<D>(p, bf, seq, head, a0 + a, lane, yy[a]);
       }
 #pragma unroll
       for (int a4 = 0; a4 < 4; ++a4) {
@@ -1113,11 +1147,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
       }
     }
     more = cursor_next(p, cur, lane, nx);
-    if (more) nx.begins = b.ends;
-    const bool any = (b.valid0 | b.valid1) != 0;
+    begins = b.ends;
+    const bool any = b.valid != 0;
     landed(b, bar_k, phase_k);
     float sv[QT][4];
-    const bool alive = (lane < kTile ? lane < b.valid0 : lane - kTile < b.valid1);   // token `lane` counts
+    const bool alive = (lane & (kTile - 1)) < (lane < kTile ? b.valid0() : b.valid1());   // token `lane` counts
     if (any) {
       if constexpr (EXACT) {
         kc[lane] = pg_norm_consts(st_kh, p.k.nc, lane, alive);
@@ -1174,7 +1208,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int o = 8 * (i & 1) + g;
-            if (o >= (i >> 1 ? b.valid1 : b.valid0)) sv[x][i] = -INFINITY;
+            if (o >= (i >> 1 ? b.valid1() : b.valid0())) sv[x][i] = -INFINITY;
             mx = fmaxf(mx, sv[x][i]);
           }
 #pragma unroll
@@ -1204,7 +1238,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
       if (any) {
         vc[lane] = pg_norm_consts(st_vh, p.v.nc, lane, alive);
         __syncwarp();
-        const int tokens = b.valid1 > 0 ? kBatch : kTile;
+        const int tokens = b.half(1) ? kBatch : kTile;
         switch (p.v.nc) {
           case 0: values(tokens, IC<0>{}); break;
           case 1: values(tokens, IC<1>{}); break;
@@ -1235,67 +1269,48 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         vc[lane] = f2;
         vd[lane] = d2;
         __syncwarp();
-        // softmax (base 2) against the whole number above the largest score so far; the weights
-        // times V's factors over a power of two that keeps the largest so far below 2^14
-        uint32_t w1[QT][2], w2[QT][2];
+        // softmax (base 2) against the whole number above the largest score so far
+        float pr[QT][4], fix[QT];
+        bool moved = false;
+        if (!b.full()) {
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int o = 8 * (i & 1) + g;
+              if (o >= (i >> 1 ? b.valid1() : b.valid0())) sv[x][i] = -INFINITY;
+            }
+        }
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int o = 8 * (i & 1) + g;
-            if (o >= (i >> 1 ? b.valid1 : b.valid0)) sv[x][i] = -INFINITY;
-            mx = fmaxf(mx, sv[x][i]);
-          }
+          float mx = max3(fmaxf(sv[x][0], sv[x][1]), sv[x][2], sv[x][3]);
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
           const float mn = fmaxf(m_[x], ceilf(mx)), ref = mn == -INFINITY ? 0.f : mn;
-          float wa[4], wb[4], wm = 0.f;
-          const float fix = ex2_approx(m_[x] - ref);         // a whole power of two, or 0
+          fix[x] = ex2_ftz(m_[x] - ref);           // a whole power of two, or 0
+          moved |= mn > m_[x];
+          m_[x] = mn;
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float pr = ex2_approx(sv[x][i] - ref);
-            const float2 f = vc[16 * (i >> 1) + 8 * (i & 1) + g];
-            sum += pr;
-            wa[i] = pr * f.x;
-            wb[i] = pr * f.y;
-            wm = fmaxf(wm, fmaxf(wa[i], wb[i]));
+            pr[x][i] = ex2_ftz(sv[x][i] - ref);
+            sum += pr[x][i];
           }
-          l_[x] = __fmaf_rn(l_[x], fix, sum);
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-          const int ex = max(ae[x], min(pg_exp_of(wm) - 13, 126));
-          const bool moved = mn > m_[x] || ex > ae[x];
-          if (__any_sync(0xffffffffu, moved)) {
-            const float f = fix * (ex > ae[x] + 252 ? 0.f : pg_exp2i((ae[x] - ex) / 2) * pg_exp2i((ae[x] - ex) - (ae[x] - ex) / 2));
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) am[x][m][i] *= f;
-          }
-          m_[x] = mn;
-          ae[x] = ex;
-          const float sc = pg_exp2i(-ex);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            w1[x][i] = h2_bits(__floats2half2_rn(wa[2 * i] * sc, wa[2 * i + 1] * sc));
-            w2[x][i] = h2_bits(__floats2half2_rn(wb[2 * i] * sc, wb[2 * i + 1] * sc));
-          }
+          l_[x] = __fmaf_rn(l_[x], fix[x], sum);
         }
         switch (p.v.nc) {
-          case 0: values_mma(w1, w2, IC<0>{}, IC<0>{}); break;
+          case 0: values_mma(pr, fix, moved, IC<0>{}, IC<0>{}); break;
           case 1:                                  // the usual values: 4-bit norms in log space
-            if (p.v.w == 6) values_mma(w1, w2, IC<1>{}, IC<6>{});
-            else if (p.v.w == 8) values_mma(w1, w2, IC<1>{}, IC<8>{});
-            else values_mma(w1, w2, IC<1>{}, IC<0>{});
+            if (p.v.w == 6) values_mma(pr, fix, moved, IC<1>{}, IC<6>{});
+            else if (p.v.w == 8) values_mma(pr, fix, moved, IC<1>{}, IC<8>{});
+            else values_mma(pr, fix, moved, IC<1>{}, IC<0>{});
             break;
           case 2:
-            if (p.v.w == 6) values_mma(w1, w2, IC<2>{}, IC<6>{});
-            else values_mma(w1, w2, IC<2>{}, IC<0>{});
+            if (p.v.w == 6) values_mma(pr, fix, moved, IC<2>{}, IC<6>{});
+            else values_mma(pr, fix, moved, IC<2>{}, IC<0>{});
             break;
-          case 3: values_mma(w1, w2, IC<3>{}, IC<0>{}); break;
-          default: values_mma(w1, w2, IC<4>{}, IC<0>{}); break;
+          case 3: values_mma(pr, fix, moved, IC<3>{}, IC<0>{}); break;
+          default: values_mma(pr, fix, moved, IC<4>{}, IC<0>{}); break;
         }
         __syncwarp();                              // every lane is done with the V rows
       }
@@ -1349,10 +1364,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
           float y[E];
 #pragma unroll
           for (int k = 0; k < E; ++k) y[k] = r[2 + E * lane + k];
-          pg_store_out<D>(p, bf, b.seq, b.head, a, lane, y, r[1]);
+          pg_store_out<D>(p, bf, seq, head, a, lane, y, r[1]);
         }
       } else if (lane == 0) {
-        sh.part[warp][begun] = b.seq * p.pg.heads + b.head;
+        sh.part[warp][begun] = seq * p.pg.heads + head;
         if (!begun) sh.ends0[warp] = b.last;
       }
     }

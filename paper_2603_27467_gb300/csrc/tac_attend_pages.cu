@@ -287,6 +287,10 @@ __device__ __forceinline__ bool cursor_next(const AttPagesParams& p, Cursor& c, 
 // cores (fp32 queries); otherwise fp16 products on the tensor cores.
 template <int D, int QT, bool EXACT>
 struct Pg {
+  // Warps of a CTA at most: 16 leave 128 registers a thread, which the accumulators of more than four
+  // queries exceed but for fp16 products at d = 64.  7 caches of 32768 tokens, 8 queries: fp16
+  // products 212 us with 16 warps, 158 with 12 (d = 64: 107 and 115), fp32 476 and 307 (213 and 184).
+  static constexpr int WARPS = QT == 1 || (D == 64 && !EXACT) ? kMaxWarps : 12;
   static constexpr int P = D / 2, NQ = 4 * QT, E = D / 32;
   static constexpr int KP = P / 4;                 // K: positions of a token a lane takes (4 lanes a token)
   static constexpr int KS = KP / 2;                // K: mma steps of a tile
@@ -496,17 +500,22 @@ __device__ __forceinline__ float2 pg_norm_consts(const uint8_t* hdr, int nc, int
   return make_float2(h.y > h.x ? (h.y - h.x) * inv : 0.f, h.x);
 }
 
-// r^ of position j of a run whose norm codes (or fp32 norms) are in w.
+// r^ of positions j and j + 1 of a run whose norm codes (or fp32 norms) are in w.
 template <int NC>
-__device__ __forceinline__ float pg_norm(const uint32_t* w, int j, float2 ab) {
+__device__ __forceinline__ float2 pg_norm2(const uint32_t* w, int j, float2 ab) {
   if constexpr (NC == 4) {
-    return ab.x != 0.f ? __uint_as_float(w[j]) : 0.f;
+    return ab.x != 0.f ? make_float2(__uint_as_float(w[j]), __uint_as_float(w[j + 1])) : make_float2(0.f, 0.f);
   } else {
-    float c;
-    if constexpr (NC >= 2) c = __uint_as_float(__byte_perm(w[j >> 2], 0x4B000000u, 0x7540 | (j & 3))) - 8388608.f;
-    else c = __uint_as_float(((w[j >> 3] >> (4 * (j & 7))) & 15u) | 0x4B000000u) - 8388608.f;
-    const float r = __fmaf_rn(c, ab.x, ab.y);
-    return NC & 1 ? ex2_ftz(r) : r;
+    float2 c;                                      // 2^23 + code
+    if constexpr (NC >= 2) {
+      c.x = __uint_as_float(__byte_perm(w[j >> 2], 0x4B000000u, 0x7540 | (j & 3)));
+      c.y = __uint_as_float(__byte_perm(w[j >> 2], 0x4B000000u, 0x7540 | ((j + 1) & 3)));
+    } else {
+      c.x = __uint_as_float(((w[j >> 3] >> (4 * (j & 7))) & 15u) | 0x4B000000u);
+      c.y = __uint_as_float(((w[j >> 3] >> (4 * ((j + 1) & 7))) & 15u) | 0x4B000000u);
+    }
+    const float2 r = ffma2(add2(c, make_float2(-8388608.f, -8388608.f)), make_float2(ab.x, ab.x), make_float2(ab.y, ab.y));
+    return NC & 1 ? make_float2(ex2_ftz(r.x), ex2_ftz(r.y)) : r;
   }
 }
 
@@ -593,7 +602,7 @@ __device__ __forceinline__ uint32_t pg_log_consts(float2 h, int nc, float& facto
 }
 
 template <int D, int QT, bool EXACT>
-__global__ void __launch_bounds__(kMaxWarps * 32, 1)
+__global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     attend_pages_kernel(const __grid_constant__ AttPagesParams p, int tab_v, int warp_bytes) {
   using C = Pg<D, QT, EXACT>;
   constexpr int NQ = C::NQ, E = C::E, KP = C::KP, KS = C::KS, VL = C::VL, VT = C::VT, VP = C::VP, MT = C::MT;
@@ -752,14 +761,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         for (int j = 0; j < 8; j += 2) {
           float2 y[2][2];
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
+          for (int r = 0; r < 2; ++r) {
+            const float2 rn = pg_norm2<NC>(nr[r], j, ab[r]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const uint32_t o = (pg_rotr(ca[r][(j + i) >> 2], (wk * ((j + i) & 3) - kTabShift) & 31) & km) | lane_off;
               const float2 cs = *reinterpret_cast<const float2*>(tk + o);
-              const float rr = pg_norm<NC>(nr[r], j + i, ab[r]);
+              const float rr = i ? rn.y : rn.x;
               y[r][i] = mul2(cs, make_float2(rr, rr));
             }
+          }
 #pragma unroll
           for (int a = 0; a < NQ; ++a) {
             const float4 q = qr[a * (4 * C::QRUN / 16) + j / 2];
@@ -794,13 +805,15 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
   const int vl = lane % VL, vt = lane / VL;
   auto values = [&](int tokens, auto nc_) {
     constexpr int NC = decltype(nc_)::value;
-    const int wv = p.v.w, bit = 4 * vl * wv, woff = (bit >> 5) * 4, wsh = bit & 31;
+    constexpr int vnb = NC == 4 ? 4 * C::P : C::P * (NC <= 1 ? 4 : 8) / 8;
+    const int wv = p.v.w, bit = 4 * vl * wv, wsh = bit & 31;
+    const uint8_t* arow = st_v + vt * p.v.ab + (bit >> 5) * 4;
+    const uint8_t* nrow = st_vn + vt * vnb;
 #pragma unroll 1
-    for (int tok = vt; tok < tokens; tok += VT) {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(st_v + tok * p.v.ab + woff);
+    for (int tok = vt; tok < tokens; tok += VT, arow += VT * p.v.ab, nrow += VT * vnb) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(arow);
       const uint32_t ca = __funnelshift_r(w[0], w[1], wsh);
       const float2 ab = vc[tok];
-      const uint8_t* nrow = st_vn + tok * p.v.nb;
       uint32_t nr[4];
       if constexpr (NC == 4) {
         const uint4 u = *reinterpret_cast<const uint4*>(nrow + 16 * vl);
@@ -816,11 +829,14 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1)
         const float4 v = *reinterpret_cast<const float4*>(wt + tok * NQ + 4 * x);
         pr[4 * x] = v.x; pr[4 * x + 1] = v.y; pr[4 * x + 2] = v.z; pr[4 * x + 3] = v.w;
       }
+      float2 rn[2];
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) rn[j / 2] = pg_norm2<NC>(nr, j, ab);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t o = (pg_rotr(ca, (wv * j - kTabShift) & 31) & vm) | lane_off;
         const float2 cs = *reinterpret_cast<const float2*>(tv + o);
-        const float rr = pg_norm<NC>(nr, j, ab);
+        const float rr = j & 1 ? rn[j / 2].y : rn[j / 2].x;
         const float2 y = mul2(cs, make_float2(rr, rr));
 #pragma unroll
         for (int a = 0; a < NQ; ++a) acc[a][j] = ffma2(y, make_float2(pr[a], pr[a]), acc[a][j]);
@@ -1492,7 +1508,7 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   const int tab_v = p.k.n == p.v.n ? 0 : (1 << p.k.w) << kTabShift;
   const int tabs = tab_v + ((1 << p.v.w) << kTabShift);
   const int warp_bytes = (C::W_STG + pg_stage_bytes(p.k) + pg_stage_bytes(p.v) + 127) / 128 * 128;
-  const int nw = std::min(kMaxWarps, (227 * 1024 - (int)sizeof(PgShared) - 256 - tabs) / warp_bytes);
+  const int nw = std::min((int)C::WARPS, (227 * 1024 - (int)sizeof(PgShared) - 256 - tabs) / warp_bytes);
   kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, tab_v, warp_bytes);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;

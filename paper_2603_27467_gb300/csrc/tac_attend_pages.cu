@@ -403,13 +403,18 @@ static_assert((int64_t)kMaxWarps * kAttPgMaxCtas * kMaxWarps * kAttPgMaxCtas < (
 __device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, int nw, Cursor& c) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = nw * 32;
   const int items = p.items, mult = p.selected ? 1 : p.pg.heads;
-  const bool few = items <= 32;                    // every warp by itself, an item a lane
-  const int chunk = few ? 1 : (items + nt - 1) / nt;
-  int mine = 0;                                    // tiles of this lane's (thread's) items
+  constexpr int LANE = 8;                          // items of a lane
+  const bool few = items <= 32 * LANE;             // every warp by itself
+  const int chunk = few ? (items + 31) / 32 : (items + nt - 1) / nt;
+  const int lo0 = (few ? lane : tid) * chunk, hi0 = min(items, lo0 + chunk);
+  int mine = 0, own[LANE];                         // tiles of this lane's (thread's) items
   if (few) {
-    if (lane < items) mine = pg_tiles(p, lane) * mult;
+#pragma unroll
+    for (int k = 0; k < LANE; ++k) own[k] = lo0 + k < hi0 ? pg_tiles(p, lo0 + k) : 0;
+#pragma unroll
+    for (int k = 0; k < LANE; ++k) mine += own[k] * mult;
   } else {
-    for (int i = tid * chunk; i < min(items, (tid + 1) * chunk); ++i) mine += pg_tiles(p, i) * mult;
+    for (int i = lo0; i < hi0; ++i) mine += pg_tiles(p, i) * mult;
   }
   int x = mine;
 #pragma unroll
@@ -435,17 +440,20 @@ __device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, i
   const int warps = min(nw, max(1, (total + 2 * p.ctas - 1) / (2 * p.ctas)));
   const int nc = min(p.ctas, (total + 2 * warps - 1) / (2 * warps)), W = nc * warps;
   if (blockIdx.x == 0 && (!few || warp == 0)) {    // for the second kernel
-    const int who = few ? lane : tid;
+    int first = at;
     if (few) {
-      if (lane < items) p.plan[lane] = at;
+#pragma unroll
+      for (int k = 0; k < LANE; ++k) {
+        if (lo0 + k < hi0) p.plan[lo0 + k] = first;
+        first += own[k] * mult;
+      }
     } else {
-      int first = at;
-      for (int i = who * chunk; i < min(items, (who + 1) * chunk); ++i) {
+      for (int i = lo0; i < hi0; ++i) {
         p.plan[i] = first;
         first += pg_tiles(p, i) * mult;
       }
     }
-    if (who == 0) {
+    if (lo0 == 0) {
       p.plan[items] = total;
       p.plan[items + 1] = nc;
       p.plan[items + 2] = warps;
@@ -461,9 +469,20 @@ __device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, i
   if (c.left <= 0) return true;
   int i, n;
   if (few) {
-    i = __ffs(__ballot_sync(0xffffffffu, x > t0)) - 1;
-    t0 -= __shfl_sync(0xffffffffu, at, i);
-    n = __shfl_sync(0xffffffffu, mine, i) / mult;
+    const int l = __ffs(__ballot_sync(0xffffffffu, x > t0)) - 1;   // the lane whose items hold tile t0
+    int rest = t0 - at, k0 = 0, n0 = 0;            // (in lane l)
+    bool in = false;
+#pragma unroll
+    for (int k = 0; k < LANE; ++k)
+      if (!in) {
+        k0 = k;
+        n0 = own[k];
+        in = rest < own[k] * mult;
+        rest -= in ? 0 : own[k] * mult;
+      }
+    t0 = __shfl_sync(0xffffffffu, rest, l);
+    n = __shfl_sync(0xffffffffu, n0, l);
+    i = __shfl_sync(0xffffffffu, lo0 + k0, l);
   } else {
     int lo = 0, hi = nt - 1;                       // the thread whose items hold tile t0
     while (lo < hi) {

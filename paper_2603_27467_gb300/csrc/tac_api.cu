@@ -1231,7 +1231,7 @@ int64_t tac_attend_pages_workspace_bytes(const tac_attend_pages_args* args) {
   const int sms = num_sms();
   if (sms <= 0) { fail(TAC_E_CUDA, "%s: no CUDA device", who); return -1; }
   ok();
-  return attend_pages_bytes(args, tac::attend_pages_ctas(args->cfg_k.d, args->dtype, args->group, sms));
+  return attend_pages_bytes(args, tac::attend_pages_ctas(sms));
 }
 
 int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t workspace_bytes, tac_stream_t stream) {
@@ -1242,7 +1242,7 @@ int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t
   if (g.seqs == 0) return ok();
   const int sms = num_sms();
   if (sms <= 0) return fail(TAC_E_CUDA, "%s: no CUDA device", who);
-  const int d = args->cfg_k.d, ctas = tac::attend_pages_ctas(d, args->dtype, args->group, sms);
+  const int ctas = tac::attend_pages_ctas(sms);
   const int64_t need = attend_pages_bytes(args, ctas);
   if (!workspace || !aligned16(workspace) || workspace_bytes < need)
     return fail(TAC_E_INVAL, "%s: workspace NULL, misaligned or smaller than %lld bytes", who, (long long)need);
@@ -1265,7 +1265,10 @@ int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t
   P.items = attend_pages_items(args);
   P.plan = static_cast<int32_t*>(workspace);
   P.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attend_pages_plan_bytes(args));
-  const cudaError_t e = tac::launch_attend_pages(d, args->dtype, P, reinterpret_cast<cudaStream_t>(stream));
+  const bool bf = args->dtype == TAC_BF16;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = args->cfg_k.d == 128 ? (bf ? tac::launch_attend_pages_128_bf16(P, st) : tac::launch_attend_pages_128_f32(P, st))
+                                             : (bf ? tac::launch_attend_pages_64_bf16(P, st) : tac::launch_attend_pages_64_f32(P, st));
   if (e != cudaSuccess) return fail(TAC_E_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   return ok();
 }

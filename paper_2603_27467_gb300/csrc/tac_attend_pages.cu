@@ -620,7 +620,13 @@ __device__ __forceinline__ uint32_t pg_log_consts(float2 h, int nc, float& facto
   return h2_bits(__halves2half2(slope, off));
 }
 
-template <int D, int QT, bool EXACT>
+// BOOKS: the norms' storage where it is known at compile time (the framework's two schemes: keys in 8
+// bits, values in 4 bits of log space or in 8 bits), kAnyBooks otherwise.  One scheme's code alone takes
+// 5 % less time than the same code among all others (32 caches of 32768 tokens 456 us against 481:
+// fewer instruction fetches wait).
+constexpr int kAnyBooks = 0, kK8V4Log = 1, kNorm8 = 2;
+
+template <int D, int QT, bool EXACT, int BOOKS>
 __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     attend_pages_kernel(const __grid_constant__ AttPagesParams p, int tab_v, int warp_bytes) {
   using C = Pg<D, QT, EXACT>;
@@ -1107,7 +1113,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     }
     return pg_exp2i(pg_exp_of(mine) + 1);
   };
-  const bool v_far = p.v.nc <= 1 && VP == 8;       // the order of the values' row tiles
+  const bool v_far = (BOOKS == kK8V4Log || (BOOKS == kAnyBooks && p.v.nc <= 1)) && VP == 8;       // the order of the values' row tiles
 
   while (more) {
     b = nx;
@@ -1150,7 +1156,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
 #pragma unroll
           for (int k = 0; k < E; k += 2) {
             const int i = pair_slot<D>((E * lane + k) / 2), r = i % KP;
-            const int at = p.k.nc <= 1 ? (r & ~7) + 2 * (r & 3) + ((r >> 2) & 1) : r;     // 4-bit norms: four apart
+            const int at = BOOKS == kAnyBooks && p.k.nc <= 1 ? (r & ~7) + 2 * (r & 3) + ((r >> 2) & 1) : r;     // 4-bit norms: four apart
             uint32_t* const w = reinterpret_cast<uint32_t*>(pw + C::W_Q) + (((at >> 2) * QT + (a >> 2)) * 32 + 8 * (a & 3) + i / KP) * 4 + (at & 3);
             const float q0 = y[k] * sc, q1 = y[k + 1] * sc;
             const __half2 hi = __floats2half2_rn(q0, q1);
@@ -1201,33 +1207,39 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       } else {
         // K's constants: linear (r_min, Delta), log (r_max, slope | offset), fp32 (2^e, 2^-e), over the
         // units of the products; zeros for a token that does not count
+        const int knc = BOOKS != kAnyBooks ? 2 : p.k.nc;
         float2 k2 = make_float2(0.f, 0.f);
-        if (p.k.nc == 4) {
+        if (knc == 4) {
           const float f = fp32_scale(st_kn, p.k.nb);
           if (alive) k2 = make_float2(f * (1.f / kUnit), 1.f / f);
         } else if (alive) {
           const float2 h = reinterpret_cast<const float2*>(st_kh)[lane];
-          if (p.k.nc & 1) {
+          if (knc & 1) {
             float f;
-            k2.y = __uint_as_float(pg_log_consts(h, p.k.nc, f));
+            k2.y = __uint_as_float(pg_log_consts(h, knc, f));
             k2.x = f * (1.f / kUnit);
           } else {
             k2.x = h.x * (1.f / kUnit);
-            k2.y = (h.y > h.x ? (h.y - h.x) * (p.k.nc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * (16777216.f / kUnit);
+            k2.y = (h.y > h.x ? (h.y - h.x) * (knc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * (16777216.f / kUnit);
           }
         }
         kc[lane] = k2;
         __syncwarp();
-        switch (p.k.nc) {
-          case 0: scores_mma(sv, IC<0>{}, IC<0>{}); break;
-          case 1: scores_mma(sv, IC<1>{}, IC<0>{}); break;
-          case 2:                                  // the usual keys: 8-bit linear norms
-            if (p.k.w == 6) scores_mma(sv, IC<2>{}, IC<6>{});
-            else if (p.k.w == 8) scores_mma(sv, IC<2>{}, IC<8>{});
-            else scores_mma(sv, IC<2>{}, IC<0>{});
-            break;
-          case 3: scores_mma(sv, IC<3>{}, IC<0>{}); break;
-          default: scores_mma(sv, IC<4>{}, IC<0>{}); break;
+        auto keys8 = [&]() {                       // 8-bit linear norms
+          if (p.k.w == 6) scores_mma(sv, IC<2>{}, IC<6>{});
+          else if (p.k.w == 8) scores_mma(sv, IC<2>{}, IC<8>{});
+          else scores_mma(sv, IC<2>{}, IC<0>{});
+        };
+        if constexpr (BOOKS != kAnyBooks) {
+          keys8();
+        } else {
+          switch (p.k.nc) {
+            case 0: scores_mma(sv, IC<0>{}, IC<0>{}); break;
+            case 1: scores_mma(sv, IC<1>{}, IC<0>{}); break;
+            case 2: keys8(); break;
+            case 3: scores_mma(sv, IC<3>{}, IC<0>{}); break;
+            default: scores_mma(sv, IC<4>{}, IC<0>{}); break;
+          }
         }
       }
       __syncwarp();                                // every lane is done with the K rows
@@ -1287,18 +1299,19 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       landed(b, bar_v, phase_v);
       if (any) {
         // V's factors: linear (r_min, 2^24 Delta), log (., r_max) and the slope, fp32 (., 2^e) and 2^-e
+        const int vnc = BOOKS == kK8V4Log ? 1 : BOOKS == kNorm8 ? 2 : p.v.nc;
         float2 f2 = make_float2(0.f, 0.f);
         uint32_t d2 = 0u;
-        if (p.v.nc == 4) {
+        if (vnc == 4) {
           const float f = fp32_scale(st_vn, p.v.nb);
           if (alive) { f2.y = f; d2 = __float_as_uint(1.f / f); }
         } else if (alive) {
           const float2 h = reinterpret_cast<const float2*>(st_vh)[lane];
-          if (p.v.nc & 1) {
-            d2 = pg_log_consts(h, p.v.nc, f2.y);
+          if (vnc & 1) {
+            d2 = pg_log_consts(h, vnc, f2.y);
           } else {
             f2.x = h.x;
-            f2.y = (h.y > h.x ? (h.y - h.x) * (p.v.nc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * 16777216.f;
+            f2.y = (h.y > h.x ? (h.y - h.x) * (vnc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * 16777216.f;
           }
         }
         vc[lane] = f2;
@@ -1333,19 +1346,21 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
           }
           l_[x] = __fmaf_rn(l_[x], fix[x], sum);
         }
-        switch (p.v.nc) {
-          case 0: values_mma(pr, fix, moved, IC<0>{}, IC<0>{}); break;
-          case 1:                                  // the usual values: 4-bit norms in log space
-            if (p.v.w == 6) values_mma(pr, fix, moved, IC<1>{}, IC<6>{});
-            else if (p.v.w == 8) values_mma(pr, fix, moved, IC<1>{}, IC<8>{});
-            else values_mma(pr, fix, moved, IC<1>{}, IC<0>{});
-            break;
-          case 2:
-            if (p.v.w == 6) values_mma(pr, fix, moved, IC<2>{}, IC<6>{});
-            else values_mma(pr, fix, moved, IC<2>{}, IC<0>{});
-            break;
-          case 3: values_mma(pr, fix, moved, IC<3>{}, IC<0>{}); break;
-          default: values_mma(pr, fix, moved, IC<4>{}, IC<0>{}); break;
+        if constexpr (BOOKS == kK8V4Log) {
+          if (p.v.w == 6) values_mma(pr, fix, moved, IC<1>{}, IC<6>{});
+          else if (p.v.w == 8) values_mma(pr, fix, moved, IC<1>{}, IC<8>{});
+          else values_mma(pr, fix, moved, IC<1>{}, IC<0>{});
+        } else if constexpr (BOOKS == kNorm8) {
+          if (p.v.w == 6) values_mma(pr, fix, moved, IC<2>{}, IC<6>{});
+          else values_mma(pr, fix, moved, IC<2>{}, IC<0>{});
+        } else {
+          switch (p.v.nc) {
+            case 0: values_mma(pr, fix, moved, IC<0>{}, IC<0>{}); break;
+            case 1: values_mma(pr, fix, moved, IC<1>{}, IC<0>{}); break;
+            case 2: values_mma(pr, fix, moved, IC<2>{}, IC<0>{}); break;
+            case 3: values_mma(pr, fix, moved, IC<3>{}, IC<0>{}); break;
+            default: values_mma(pr, fix, moved, IC<4>{}, IC<0>{}); break;
+          }
         }
         __syncwarp();                              // every lane is done with the V rows
       }
@@ -1517,10 +1532,10 @@ static cudaError_t set_smem_once(K kp, std::atomic<int>* ready) {
   return e;
 }
 
-template <int D, int QT, bool EXACT>
+template <int D, int QT, bool EXACT, int BOOKS>
 static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   using C = Pg<D, QT, EXACT>;
-  auto kp = attend_pages_kernel<D, QT, EXACT>;
+  auto kp = attend_pages_kernel<D, QT, EXACT, BOOKS>;
   static std::atomic<int> ready[64];
   cudaError_t e = set_smem_once(kp, ready);
   if (e != cudaSuccess) return e;
@@ -1538,17 +1553,26 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-// CTAs of the main kernel: one on every SM.
-int attend_pages_ctas(int, int, int, int sms) { return std::min(sms, kAttPgMaxCtas); }
-
-cudaError_t launch_attend_pages(int d, int dtype, const AttPagesParams& p, cudaStream_t st) {
-  const bool wide = p.group > 4;
-  if (dtype == TAC_BF16) {
-    if (d == 128) return wide ? launch_pages_t<128, 2, false>(p, st) : launch_pages_t<128, 1, false>(p, st);
-    return wide ? launch_pages_t<64, 2, false>(p, st) : launch_pages_t<64, 1, false>(p, st);
+template <int D, bool EXACT>
+static cudaError_t launch_pages_d(const AttPagesParams& p, cudaStream_t st) {
+#define TAC_PAGES(BOOKS) (p.group > 4 ? launch_pages_t<D, 2, EXACT, BOOKS>(p, st) : launch_pages_t<D, 1, EXACT, BOOKS>(p, st))
+  if constexpr (!EXACT) {
+    if (p.k.nc == 2 && p.v.nc == 1) return TAC_PAGES(kK8V4Log);
+    if (p.k.nc == 2 && p.v.nc == 2) return TAC_PAGES(kNorm8);
   }
-  if (d == 128) return wide ? launch_pages_t<128, 2, true>(p, st) : launch_pages_t<128, 1, true>(p, st);
-  return wide ? launch_pages_t<64, 2, true>(p, st) : launch_pages_t<64, 1, true>(p, st);
+  return TAC_PAGES(kAnyBooks);
+#undef TAC_PAGES
 }
+
+// Each (d, type) is a translation unit of its own (the same source, compiled in parallel).
+#if TAC_INST_D == 128 && defined(TAC_INST_BF16)
+cudaError_t launch_attend_pages_128_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<128, false>(p, st); }
+#elif TAC_INST_D == 128
+cudaError_t launch_attend_pages_128_f32(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<128, true>(p, st); }
+#elif defined(TAC_INST_BF16)
+cudaError_t launch_attend_pages_64_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<64, false>(p, st); }
+#else
+cudaError_t launch_attend_pages_64_f32(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<64, true>(p, st); }
+#endif
 
 }  // namespace tac

@@ -742,7 +742,8 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
   // Scores of the staged batch: lane (g, t) takes positions KP t .. KP t + KP - 1 of tokens g and
   // g + 8 of a tile.  sv[x][i]: token 16 (i / 2) + 8 (i & 1) + g, query 4 x + t.
   auto scores = [&](float (&sv)[QT][4], auto nc_) {
-    constexpr int NC = decltype(nc_)::value;
+    constexpr int NC = decltype(nc_)::value, KB = NC <= 1 ? 4 : 8;
+    constexpr int knb = NC == 4 ? 4 * C::P : C::P * KB / 8;
     const int wk = p.k.w;
 #pragma unroll
     for (int x = 0; x < QT; ++x) sv[x][2] = sv[x][3] = 0.f;
@@ -756,29 +757,25 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       for (int a = 0; a < NQ; ++a) s[a][0] = s[a][1] = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int q8 = 0; q8 < KP / 8; ++q8) {
-        uint32_t ca[2][2], nr[2][NC == 4 ? 8 : 2];
+        Run<0, 8> run[2];
+        uint32_t nr[2][NC == 4 ? 8 : 2];
         float2 ab[2];
+        const int bit = (KP * t + 8 * q8) * wk;
+        const uint8_t* arow = st_k + (kTile * hf + g) * p.k.ab + (bit >> 5) * 4;
+        const uint8_t* nrow = st_kn + (kTile * hf + g) * knb + (NC == 4 ? 4 : KB) * (KP * t + 8 * q8) / (NC == 4 ? 1 : 8);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int tok = kTile * hf + 8 * r + g;
-          const int off = tok * p.k.ab + (t * (KP / 8) + q8) * wk;     // 8 codes: wk bytes
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(st_k + (off & ~3));
-          const int sh_ = (off & 3) * 8;
-          const uint32_t w0 = w[0], w1 = w[1], w2 = w[2];
-          ca[r][0] = __funnelshift_r(w0, w1, sh_);
-          ca[r][1] = __funnelshift_rc(ca[r][0], __funnelshift_r(w1, w2, sh_), 4 * wk);
-          ab[r] = kc[tok];
-          const uint8_t* nrow = st_kn + tok * p.k.nb;
-          const int p0 = KP * t + 8 * q8;
+        for (int r = 0; r < 2; ++r, arow += 8 * p.k.ab, nrow += 8 * knb) {
+          run[r].load(arow, bit & 31, wk);
+          ab[r] = kc[kTile * hf + 8 * r + g];
           if constexpr (NC == 4) {
-            const uint4 u = *reinterpret_cast<const uint4*>(nrow + 4 * p0), v = *reinterpret_cast<const uint4*>(nrow + 4 * p0 + 16);
+            const uint4 u = *reinterpret_cast<const uint4*>(nrow), v = *reinterpret_cast<const uint4*>(nrow + 16);
             nr[r][0] = u.x; nr[r][1] = u.y; nr[r][2] = u.z; nr[r][3] = u.w;
             nr[r][4] = v.x; nr[r][5] = v.y; nr[r][6] = v.z; nr[r][7] = v.w;
           } else if constexpr (NC >= 2) {
-            const uint2 u = *reinterpret_cast<const uint2*>(nrow + p0);
+            const uint2 u = *reinterpret_cast<const uint2*>(nrow);
             nr[r][0] = u.x; nr[r][1] = u.y;
           } else {
-            nr[r][0] = *reinterpret_cast<const uint32_t*>(nrow + p0 / 2);
+            nr[r][0] = *reinterpret_cast<const uint32_t*>(nrow);
           }
         }
         const float4* qr = reinterpret_cast<const float4*>(pw + C::W_Q + t * C::QRUN + q8 * 64);
@@ -790,7 +787,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
             const float2 rn = pg_norm2<NC>(nr[r], j, ab[r]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const uint32_t o = (pg_rotr(ca[r][(j + i) >> 2], (wk * ((j + i) & 3) - kTabShift) & 31) & km) | lane_off;
+              const uint32_t o = (run[r].offset(j + i, wk) & km) | lane_off;
               const float2 cs = *reinterpret_cast<const float2*>(tk + o);
               const float rr = i ? rn.y : rn.x;
               y[r][i] = mul2(cs, make_float2(rr, rr));
@@ -1195,14 +1192,18 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     const bool alive = (lane & (kTile - 1)) < (lane < kTile ? b.valid0() : b.valid1());   // token `lane` counts
     if (any) {
       if constexpr (EXACT) {
-        kc[lane] = pg_norm_consts(st_kh, p.k.nc, lane, alive);
+        kc[lane] = pg_norm_consts(st_kh, BOOKS != kAnyBooks ? 2 : p.k.nc, lane, alive);
         __syncwarp();
-        switch (p.k.nc) {
-          case 0: scores(sv, IC<0>{}); break;
-          case 1: scores(sv, IC<1>{}); break;
-          case 2: scores(sv, IC<2>{}); break;
-          case 3: scores(sv, IC<3>{}); break;
-          default: scores(sv, IC<4>{}); break;
+        if constexpr (BOOKS != kAnyBooks) {
+          scores(sv, IC<2>{});
+        } else {
+          switch (p.k.nc) {
+            case 0: scores(sv, IC<0>{}); break;
+            case 1: scores(sv, IC<1>{}); break;
+            case 2: scores(sv, IC<2>{}); break;
+            case 3: scores(sv, IC<3>{}); break;
+            default: scores(sv, IC<4>{}); break;
+          }
         }
       } else {
         // K's constants: linear (r_min, Delta), log (r_max, slope | offset), fp32 (2^e, 2^-e), over the
@@ -1283,15 +1284,19 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       }
       landed(b, bar_v, phase_v);
       if (any) {
-        vc[lane] = pg_norm_consts(st_vh, p.v.nc, lane, alive);
+        vc[lane] = pg_norm_consts(st_vh, BOOKS == kK8V4Log ? 1 : BOOKS == kNorm8 ? 2 : p.v.nc, lane, alive);
         __syncwarp();
         const int tokens = b.half(1) ? kBatch : kTile;
-        switch (p.v.nc) {
-          case 0: values(tokens, IC<0>{}); break;
-          case 1: values(tokens, IC<1>{}); break;
-          case 2: values(tokens, IC<2>{}); break;
-          case 3: values(tokens, IC<3>{}); break;
-          default: values(tokens, IC<4>{}); break;
+        if constexpr (BOOKS != kAnyBooks) {
+          values(tokens, IC<BOOKS == kK8V4Log ? 1 : 2>{});
+        } else {
+          switch (p.v.nc) {
+            case 0: values(tokens, IC<0>{}); break;
+            case 1: values(tokens, IC<1>{}); break;
+            case 2: values(tokens, IC<2>{}); break;
+            case 3: values(tokens, IC<3>{}); break;
+            default: values(tokens, IC<4>{}); break;
+          }
         }
         __syncwarp();                              // every lane is done with the V rows
       }
@@ -1556,10 +1561,8 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
 template <int D, bool EXACT>
 static cudaError_t launch_pages_d(const AttPagesParams& p, cudaStream_t st) {
 #define TAC_PAGES(BOOKS) (p.group > 4 ? launch_pages_t<D, 2, EXACT, BOOKS>(p, st) : launch_pages_t<D, 1, EXACT, BOOKS>(p, st))
-  if constexpr (!EXACT) {
-    if (p.k.nc == 2 && p.v.nc == 1) return TAC_PAGES(kK8V4Log);
-    if (p.k.nc == 2 && p.v.nc == 2) return TAC_PAGES(kNorm8);
-  }
+  if (p.k.nc == 2 && p.v.nc == 1) return TAC_PAGES(kK8V4Log);
+  if (p.k.nc == 2 && p.v.nc == 2) return TAC_PAGES(kNorm8);
   return TAC_PAGES(kAnyBooks);
 #undef TAC_PAGES
 }

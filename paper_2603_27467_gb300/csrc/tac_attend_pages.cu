@@ -26,6 +26,7 @@ struct IC { static constexpr int value = V; };
 constexpr float kPgLog2e = 1.4426950408889634f;
 constexpr int kBatch = 2 * kTile;
 constexpr int kMaxWarps = 16;
+constexpr int kPlanAlone = 256;                   // up to so many items every warp plans by itself
 constexpr int kTabShift = 7;                      // log2 of a bin-centre table entry's bytes, all copies
 constexpr float kUnit = 32768.f;                  // fp16 bin centres are scaled by it
 
@@ -300,15 +301,14 @@ struct Pg {
   static constexpr int QBYTES = EXACT ? NQ * 4 * QRUN : KS * QT * 256;
   static constexpr int REC = NQ * pg_rec_floats(D) * 4;
   // per warp: rotated queries (and the record of a part that ends here) | record of a part that
-  // began in an earlier warp | the queries' scales | constants of the batch's tokens: K, V, V's
-  // exponent slopes | softmax weights (EXACT) | staging
+  // began in an earlier warp | the queries' scales | constants of the batch's tokens, K and V |
+  // softmax weights (EXACT) | staging
   static constexpr int W_Q = 0;
   static constexpr int W_REC = ((QBYTES > REC ? QBYTES : REC) + 15) / 16 * 16;
   static constexpr int W_QS = W_REC + (REC + 15) / 16 * 16;
   static constexpr int W_KC = W_QS + NQ * 4;
   static constexpr int W_VC = W_KC + kBatch * 8;
-  static constexpr int W_VD = W_VC + kBatch * 8;
-  static constexpr int W_P = W_VD + (EXACT ? 0 : kBatch * 4);
+  static constexpr int W_P = W_VC + kBatch * 8;
   static constexpr int W_STG = W_P + (EXACT ? kBatch * NQ * 4 : 0);
   static_assert(W_KC % 16 == 0 && W_STG % 16 == 0, "layout");
 };
@@ -317,7 +317,6 @@ __host__ __device__ inline int pg_stage_bytes(const Book& b) { return kBatch * (
 // CTA-wide bookkeeping, in front of the dynamic shared memory.
 struct PgShared {
   int64_t bars[2 * kMaxWarps];                     // mbarriers: K, V of each warp
-  int pref[kMaxWarps * 32];                        // first tile of each thread's items
   int scan[kMaxWarps];
   // parts: what each warp left.  0: one that began in an earlier warp, 1: one that begins
   // here and goes on.  -1: none; seq * heads + head otherwise.
@@ -325,6 +324,8 @@ struct PgShared {
   int ends0[kMaxWarps];                            // part 0 ends in this warp
   int empty[kMaxWarps];                            // no tiles
 };
+
+constexpr int kDynamic = 227 * 1024 - (int)(sizeof(PgShared) + 127) / 128 * 128;   // what it leaves of an SM's memory
 
 // Joins of a CTA's parts: every (chain of parts, query) is one warp's task.  A chain starts with a part
 // that begins in its warp, or with the CTA's first part, and goes on through the warps whose first
@@ -400,11 +401,12 @@ __device__ __forceinline__ int pg_start(int total, int w, int W) {
   return q * w + (int)((uint32_t)(r * w) / (uint32_t)W);       // r w < W^2, W <= 16 * kAttPgMaxCtas
 }
 static_assert((int64_t)kMaxWarps * kAttPgMaxCtas * kMaxWarps * kAttPgMaxCtas < (int64_t)1 << 31, "pg_start");
-__device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, int nw, Cursor& c) {
+// pref: a word a thread, free until the tables are filled.
+__device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, int* pref, int nw, Cursor& c) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = nw * 32;
   const int items = p.items, mult = p.selected ? 1 : p.pg.heads;
-  constexpr int LANE = 8;                          // items of a lane
-  const bool few = items <= 32 * LANE;             // every warp by itself
+  constexpr int LANE = kPlanAlone / 32;            // items of a lane
+  const bool few = items <= kPlanAlone;            // every warp by itself
   const int chunk = few ? (items + 31) / 32 : (items + nt - 1) / nt;
   const int lo0 = (few ? lane : tid) * chunk, hi0 = min(items, lo0 + chunk);
   int mine = 0, own[LANE];                         // tiles of this lane's (thread's) items
@@ -433,7 +435,7 @@ __device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, i
       if (w == warp) at += total;
       total += sh.scan[w];
     }
-    sh.pref[tid] = at;
+    pref[tid] = at;
     __syncthreads();
   }
   // at least two tiles a warp, and all CTAs before many warps of each
@@ -487,9 +489,9 @@ __device__ __forceinline__ bool pg_plan(const AttPagesParams& p, PgShared& sh, i
     int lo = 0, hi = nt - 1;                       // the thread whose items hold tile t0
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (sh.pref[mid] <= t0) lo = mid; else hi = mid - 1;
+      if (pref[mid] <= t0) lo = mid; else hi = mid - 1;
     }
-    t0 -= sh.pref[lo];
+    t0 -= pref[lo];
     i = lo * chunk;
     n = pg_tiles(p, i);
     while (t0 >= n * mult) {
@@ -561,7 +563,7 @@ struct Run {
 #pragma unroll
           for (int i = 0; i < NW; ++i) x[i] = p[i];
         }
-      } else {                                     // W = 6: the run ends inside its last word
+      } else {                                     // the run ends inside its last word
         uint32_t a = p[0];
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
@@ -649,7 +651,6 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
   uint8_t* const st_vh = st_vn + kBatch * p.v.nb;
   float2* const kc = reinterpret_cast<float2*>(pw + C::W_KC);
   float2* const vc = reinterpret_cast<float2*>(pw + C::W_VC);
-  uint32_t* const vd = reinterpret_cast<uint32_t*>(pw + C::W_VD);  // mma: (slope, offset) of V's log2 norms, two halves
   float* const wt = reinterpret_cast<float*>(pw + C::W_P);       // EXACT: [token][query]
   auto rec_of = [&](int w, int which) {
     return reinterpret_cast<float*>(pool + w * warp_bytes + (which ? C::W_Q : C::W_REC));
@@ -664,7 +665,9 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     sh.ends0[warp] = 0;
   }
   Cursor cur;
-  if (!pg_plan(p, sh, nw, cur)) return;            // no tile for this CTA
+  // (a plan's words lie where the tables will be: 2 KB at least, with the warps' memory behind them)
+  if (!pg_plan(p, sh, reinterpret_cast<int*>(smem), nw, cur)) return;   // no tile for this CTA
+  if (p.items > kPlanAlone) __syncthreads();       // every warp has found its place
   if (lane == 0) sh.empty[warp] = cur.left <= 0;
 
   // ---- staging: one lane (elected, so that the compiler knows it is one) copies the planes (angle | norm | header) of a batch's tiles, both at
@@ -976,7 +979,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     const int wv = W ? W : p.v.w, vab = W ? C::P * W / 8 : p.v.ab, vbit = VP * g * wv;
     const uint8_t* arow = st_v + t * vab + (vbit >> 5) * 4;
     const uint8_t* nrow = st_vn + t * vnb + (F32N ? 4 * VP * g : VP * VB * g / 8);
-    const uint32_t* cst = vd + t;
+    const float2* cst = vc + t;
     uint32_t w1[QT][2], w2[QT][2];
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
@@ -1028,7 +1031,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
           const int row = 8 * s8 + 4 * i;          // of this tile, behind token t
           run[i].load(arow + row * vab, vbit & 31, wv);
           const uint8_t* nr = nrow + row * vnb;
-          sl[i] = cst[row];
+          sl[i] = __float_as_uint(cst[row].x);     // log: slope and offset; fp32: 2^-e
           if constexpr (F32N) {
           } else if constexpr (VW == 2) {
             const uint2 v = *reinterpret_cast<const uint2*>(nr);
@@ -1228,6 +1231,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
         __syncwarp();
         auto keys8 = [&]() {                       // 8-bit linear norms
           if (p.k.w == 6) scores_mma(sv, IC<2>{}, IC<6>{});
+          else if (p.k.w == 7) scores_mma(sv, IC<2>{}, IC<7>{});
           else if (p.k.w == 8) scores_mma(sv, IC<2>{}, IC<8>{});
           else scores_mma(sv, IC<2>{}, IC<0>{});
         };
@@ -1303,24 +1307,22 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     } else {
       landed(b, bar_v, phase_v);
       if (any) {
-        // V's factors: linear (r_min, 2^24 Delta), log (., r_max) and the slope, fp32 (., 2^e) and 2^-e
+        // V's factors: linear (r_min, 2^24 Delta), log (slope | offset, r_max), fp32 (2^-e, 2^e)
         const int vnc = BOOKS == kK8V4Log ? 1 : BOOKS == kNorm8 ? 2 : p.v.nc;
         float2 f2 = make_float2(0.f, 0.f);
-        uint32_t d2 = 0u;
         if (vnc == 4) {
           const float f = fp32_scale(st_vn, p.v.nb);
-          if (alive) { f2.y = f; d2 = __float_as_uint(1.f / f); }
+          if (alive) f2 = make_float2(1.f / f, f);
         } else if (alive) {
           const float2 h = reinterpret_cast<const float2*>(st_vh)[lane];
           if (vnc & 1) {
-            d2 = pg_log_consts(h, vnc, f2.y);
+            f2.x = __uint_as_float(pg_log_consts(h, vnc, f2.y));
           } else {
             f2.x = h.x;
             f2.y = (h.y > h.x ? (h.y - h.x) * (vnc == 2 ? 1.f / 255.f : 1.f / 15.f) : 0.f) * 16777216.f;
           }
         }
         vc[lane] = f2;
-        vd[lane] = d2;
         __syncwarp();
         // softmax (base 2) against the whole number above the largest score so far
         float pr[QT][4], fix[QT];
@@ -1353,10 +1355,12 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
         }
         if constexpr (BOOKS == kK8V4Log) {
           if (p.v.w == 6) values_mma(pr, fix, moved, IC<1>{}, IC<6>{});
+          else if (p.v.w == 7) values_mma(pr, fix, moved, IC<1>{}, IC<7>{});
           else if (p.v.w == 8) values_mma(pr, fix, moved, IC<1>{}, IC<8>{});
           else values_mma(pr, fix, moved, IC<1>{}, IC<0>{});
         } else if constexpr (BOOKS == kNorm8) {
           if (p.v.w == 6) values_mma(pr, fix, moved, IC<2>{}, IC<6>{});
+          else if (p.v.w == 8) values_mma(pr, fix, moved, IC<2>{}, IC<8>{});
           else values_mma(pr, fix, moved, IC<2>{}, IC<0>{});
         } else {
           switch (p.v.nc) {
@@ -1532,7 +1536,7 @@ static cudaError_t set_smem_once(K kp, std::atomic<int>* ready) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (ready[dev].load(std::memory_order_acquire)) return cudaSuccess;
   // static shared memory counts towards the 227 KB
-  const cudaError_t e = cudaFuncSetAttribute(kp, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)sizeof(PgShared) - 256);
+  const cudaError_t e = cudaFuncSetAttribute(kp, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamic);
   if (e == cudaSuccess) ready[dev].store(1, std::memory_order_release);
   return e;
 }
@@ -1547,7 +1551,7 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   const int tab_v = p.k.n == p.v.n ? 0 : (1 << p.k.w) << kTabShift;
   const int tabs = tab_v + ((1 << p.v.w) << kTabShift);
   const int warp_bytes = (C::W_STG + pg_stage_bytes(p.k) + pg_stage_bytes(p.v) + 127) / 128 * 128;
-  const int nw = std::min((int)C::WARPS, (227 * 1024 - (int)sizeof(PgShared) - 256 - tabs) / warp_bytes);
+  const int nw = std::min((int)C::WARPS, (kDynamic - tabs) / warp_bytes);
   kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, tab_v, warp_bytes);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;

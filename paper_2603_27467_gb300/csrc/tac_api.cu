@@ -1267,8 +1267,12 @@ int tac_attend_pages(const tac_attend_pages_args* args, void* workspace, int64_t
   P.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attend_pages_plan_bytes(args));
   const bool bf = args->dtype == TAC_BF16;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = args->cfg_k.d == 128 ? (bf ? tac::launch_attend_pages_128_bf16(P, st) : tac::launch_attend_pages_128_f32(P, st))
-                                             : (bf ? tac::launch_attend_pages_64_bf16(P, st) : tac::launch_attend_pages_64_f32(P, st));
+  // bf16 queries take fp16 products, but over fp32 norms only from five queries a head on: rounding
+  // the norms to halves costs more than fp32 products of up to four queries (7 caches of 32768 tokens,
+  // d = 128: 318 us against 270, 8 queries 354 against 400; d = 64: 133 and 117, 147 and 172)
+  const bool half = bf && !(P.k.nc == 4 && P.v.nc == 4 && P.group <= 4);
+  const cudaError_t e = args->cfg_k.d == 128 ? (half ? tac::launch_attend_pages_128_bf16(P, st) : tac::launch_attend_pages_128_f32(P, bf, st))
+                                             : (half ? tac::launch_attend_pages_64_bf16(P, st) : tac::launch_attend_pages_64_f32(P, bf, st));
   if (e != cudaSuccess) return fail(TAC_E_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   return ok();
 }

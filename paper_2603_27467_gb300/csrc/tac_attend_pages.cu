@@ -626,16 +626,16 @@ __device__ __forceinline__ uint32_t pg_log_consts(float2 h, int nc, float& facto
 // bits, values in 4 bits of log space or in 8 bits), kAnyBooks otherwise.  One scheme's code alone takes
 // 5 % less time than the same code among all others (32 caches of 32768 tokens 456 us against 481:
 // fewer instruction fetches wait).
-constexpr int kAnyBooks = 0, kK8V4Log = 1, kNorm8 = 2;
+constexpr int kAnyBooks = 0, kK8V4Log = 1, kNorm8 = 2, kFp32Norms = 3;
 
 template <int D, int QT, bool EXACT, int BOOKS>
 __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
-    attend_pages_kernel(const __grid_constant__ AttPagesParams p, int tab_v, int warp_bytes) {
+    attend_pages_kernel(const __grid_constant__ AttPagesParams p, int bf16_rows, int tab_v, int warp_bytes) {
   using C = Pg<D, QT, EXACT>;
   constexpr int NQ = C::NQ, E = C::E, KP = C::KP, KS = C::KS, VL = C::VL, VT = C::VT, VP = C::VP, MT = C::MT;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ PgShared sh;
-  constexpr bool bf = !EXACT;                      // bf16 queries and outputs, else fp32
+  const bool bf = !EXACT || bf16_rows;             // bf16 queries and outputs, else fp32
   const int tid = threadIdx.x, lane = tid & 31, nw = blockDim.x >> 5;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int g = lane >> 2, t = lane & 3;
@@ -1195,10 +1195,10 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
     const bool alive = (lane & (kTile - 1)) < (lane < kTile ? b.valid0() : b.valid1());   // token `lane` counts
     if (any) {
       if constexpr (EXACT) {
-        kc[lane] = pg_norm_consts(st_kh, BOOKS != kAnyBooks ? 2 : p.k.nc, lane, alive);
+        kc[lane] = pg_norm_consts(st_kh, BOOKS == kAnyBooks ? p.k.nc : BOOKS == kFp32Norms ? 4 : 2, lane, alive);
         __syncwarp();
         if constexpr (BOOKS != kAnyBooks) {
-          scores(sv, IC<2>{});
+          scores(sv, IC<BOOKS == kFp32Norms ? 4 : 2>{});
         } else {
           switch (p.k.nc) {
             case 0: scores(sv, IC<0>{}); break;
@@ -1288,11 +1288,11 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       }
       landed(b, bar_v, phase_v);
       if (any) {
-        vc[lane] = pg_norm_consts(st_vh, BOOKS == kK8V4Log ? 1 : BOOKS == kNorm8 ? 2 : p.v.nc, lane, alive);
+        vc[lane] = pg_norm_consts(st_vh, BOOKS == kAnyBooks ? p.v.nc : BOOKS == kFp32Norms ? 4 : BOOKS == kK8V4Log ? 1 : 2, lane, alive);
         __syncwarp();
         const int tokens = b.half(1) ? kBatch : kTile;
         if constexpr (BOOKS != kAnyBooks) {
-          values(tokens, IC<BOOKS == kK8V4Log ? 1 : 2>{});
+          values(tokens, IC<BOOKS == kK8V4Log ? 1 : BOOKS == kNorm8 ? 2 : 4>{});
         } else {
           switch (p.v.nc) {
             case 0: values(tokens, IC<0>{}); break;
@@ -1542,7 +1542,7 @@ static cudaError_t set_smem_once(K kp, std::atomic<int>* ready) {
 }
 
 template <int D, int QT, bool EXACT, int BOOKS>
-static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
+static cudaError_t launch_pages_t(const AttPagesParams& p, bool bf, cudaStream_t st) {
   using C = Pg<D, QT, EXACT>;
   auto kp = attend_pages_kernel<D, QT, EXACT, BOOKS>;
   static std::atomic<int> ready[64];
@@ -1552,34 +1552,39 @@ static cudaError_t launch_pages_t(const AttPagesParams& p, cudaStream_t st) {
   const int tabs = tab_v + ((1 << p.v.w) << kTabShift);
   const int warp_bytes = (C::W_STG + pg_stage_bytes(p.k) + pg_stage_bytes(p.v) + 127) / 128 * 128;
   const int nw = std::min((int)C::WARPS, (kDynamic - tabs) / warp_bytes);
-  kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, tab_v, warp_bytes);
+  kp<<<p.ctas, nw * 32, tabs + nw * warp_bytes, st>>>(p, (int)bf, tab_v, warp_bytes);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   // an ordinary launch: started while the main kernel runs (programmatic dependent launch) it ended
   // 3.5 us later in calls of few tokens
   const unsigned grid = (unsigned)((int64_t)p.pg.seqs * p.pg.heads * p.group);
-  attend_pages_join<D><<<grid, kJoinWarps * 32, 0, st>>>(p, (int)!EXACT);
+  attend_pages_join<D><<<grid, kJoinWarps * 32, 0, st>>>(p, (int)bf);
   return cudaGetLastError();
 }
 
+// The codebooks' kernel.
 template <int D, bool EXACT>
-static cudaError_t launch_pages_d(const AttPagesParams& p, cudaStream_t st) {
-#define TAC_PAGES(BOOKS) (p.group > 4 ? launch_pages_t<D, 2, EXACT, BOOKS>(p, st) : launch_pages_t<D, 1, EXACT, BOOKS>(p, st))
+static cudaError_t launch_pages_d(const AttPagesParams& p, bool bf, cudaStream_t st) {
+#define TAC_PAGES(BOOKS) (p.group > 4 ? launch_pages_t<D, 2, EXACT, BOOKS>(p, bf, st) : launch_pages_t<D, 1, EXACT, BOOKS>(p, bf, st))
   if (p.k.nc == 2 && p.v.nc == 1) return TAC_PAGES(kK8V4Log);
   if (p.k.nc == 2 && p.v.nc == 2) return TAC_PAGES(kNorm8);
+  if constexpr (EXACT) {
+    if (p.k.nc == 4 && p.v.nc == 4) return TAC_PAGES(kFp32Norms);
+  }
   return TAC_PAGES(kAnyBooks);
 #undef TAC_PAGES
 }
 
-// Each (d, type) is a translation unit of its own (the same source, compiled in parallel).
+// Each (d, products) is a translation unit of its own (the same source, compiled in parallel).  fp32
+// products also serve bf16 queries (`bf`).
 #if TAC_INST_D == 128 && defined(TAC_INST_BF16)
-cudaError_t launch_attend_pages_128_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<128, false>(p, st); }
+cudaError_t launch_attend_pages_128_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<128, false>(p, true, st); }
 #elif TAC_INST_D == 128
-cudaError_t launch_attend_pages_128_f32(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<128, true>(p, st); }
+cudaError_t launch_attend_pages_128_f32(const AttPagesParams& p, bool bf, cudaStream_t st) { return launch_pages_d<128, true>(p, bf, st); }
 #elif defined(TAC_INST_BF16)
-cudaError_t launch_attend_pages_64_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<64, false>(p, st); }
+cudaError_t launch_attend_pages_64_bf16(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<64, false>(p, true, st); }
 #else
-cudaError_t launch_attend_pages_64_f32(const AttPagesParams& p, cudaStream_t st) { return launch_pages_d<64, true>(p, st); }
+cudaError_t launch_attend_pages_64_f32(const AttPagesParams& p, bool bf, cudaStream_t st) { return launch_pages_d<64, true>(p, bf, st); }
 #endif
 
 }  // namespace tac

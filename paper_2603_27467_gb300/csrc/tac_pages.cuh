@@ -83,9 +83,9 @@ constexpr int kAttPgMaxCtas = 1024;
 // CTAs of the main kernel: one on every SM.
 inline int attend_pages_ctas(int sms) { return sms < kAttPgMaxCtas ? sms : kAttPgMaxCtas; }
 cudaError_t launch_attend_pages_128_bf16(const AttPagesParams& p, cudaStream_t st);
-cudaError_t launch_attend_pages_128_f32(const AttPagesParams& p, cudaStream_t st);
+cudaError_t launch_attend_pages_128_f32(const AttPagesParams& p, bool bf, cudaStream_t st);
 cudaError_t launch_attend_pages_64_bf16(const AttPagesParams& p, cudaStream_t st);
-cudaError_t launch_attend_pages_64_f32(const AttPagesParams& p, cudaStream_t st);
+cudaError_t launch_attend_pages_64_f32(const AttPagesParams& p, bool bf, cudaStream_t st);
 
 cudaError_t launch_page_bounds(int d, int dtype, const BoundsParams& p, int sms, cudaStream_t st);
 cudaError_t launch_select_pages(int d, int dtype, const SelectParams& p, int sms, cudaStream_t st);

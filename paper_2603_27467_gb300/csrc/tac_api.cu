@@ -1124,6 +1124,8 @@ int check_attend_pages(const tac_attend_pages_args* A, const char* who) {
   if (A->capacity < 0 || g.pages > A->capacity / ((int64_t)g.kv_heads * g.page_tokens))
     return fail(TAC_E_INVAL, "%s: %lld pages of %d heads x %d tokens do not fit %lld record slots", who, (long long)g.pages,
                 g.kv_heads, g.page_tokens, (long long)A->capacity);
+  if (A->capacity > ((int64_t)1 << 35))   // places are 32-bit numbers of 16-slot tiles
+    return fail(TAC_E_UNSUPPORTED, "%s: capacity %lld is above 2^35 record slots", who, (long long)A->capacity);
   if ((A->selected == nullptr) != (A->counts == nullptr))
     return fail(TAC_E_INVAL, "%s: selected and counts come together", who);
   if (A->selected && (A->budget < 1 || !aligned4(A->selected) || !aligned4(A->counts)))

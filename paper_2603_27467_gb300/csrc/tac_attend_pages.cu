@@ -11,6 +11,19 @@
 // there; the parts of one that several warps of a CTA share are joined in shared memory in
 // the order of the warps; the parts of several CTAs go to the workspace and a second
 // kernel joins them in the order of the CTAs.
+//
+// Products: for bf16 queries on the tensor cores (mma.sync m16n8k16, fp16 operands decoded in the
+// registers of the fragments, fp32 sums); for fp32 queries packed fp32 multiply-adds.  tcgen05 takes
+// its operands from shared memory or TMEM, where the decoded values would have to be written
+// first, and the contraction is not what bounds: the tensor pipe is active 16 % of the time.
+// Bound: instruction issue.  Of 44 warp-instructions a token-head (d = 128, 4 queries, 8-bit linear K,
+// 4-bit log V, n = 64) K takes 15 and V 18 (a code's shift, mask and lookup 3, the norm and the product
+// 1.5 to 3), the rest are copies, softmax and weights, constants of the records, places of
+// the tiles; they issue in 67 % of the cycles at 16 warps an SM.  32 caches of 32768 tokens (1.69 GB):
+// 443 us, 3.8 TB/s, 56 % of the measured copy rate; the same loop without K's and V's products takes
+// 271 us (timing copy), so the copies would keep up.  With fp32 products (first form of this kernel) 957.
+// A call of one sequence of 4097 tokens takes 16.7 us: 12 in this kernel (lengths, page table, query,
+// records: four waits for memory in a row, then one batch a warp and the joins), 3.4 in the second.
 #include <algorithm>
 #include <atomic>
 
@@ -75,7 +88,6 @@ __device__ __forceinline__ bool pg_bar_wait(uint32_t bar, uint32_t parity) {
   }
   return false;
 }
-__device__ __forceinline__ void pg_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ uint32_t pg_rotr(uint32_t x, int s) { return __funnelshift_r(x, x, s); }
 __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 
@@ -670,8 +682,8 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
   if (p.items > kPlanAlone) __syncthreads();       // every warp has found its place
   if (lane == 0) sh.empty[warp] = cur.left <= 0;
 
-  // ---- staging: one lane (elected, so that the compiler knows it is one) copies the planes (angle | norm | header) of a batch's tiles, both at
-  // once where they lie side by side ----
+  // ---- staging: one lane (elected, so that the compiler knows it is one) copies the planes
+  // (angle | norm | header) of a batch's tiles, both at once where they lie side by side ----
   uint32_t phase_k = 0, phase_v = 0;
   bool dead = false;                               // a wait ran out
   auto copy_rows = [&](const Book& bk, uint32_t stage, uint32_t bar, uint32_t tile, int half, int rows) {
@@ -700,7 +712,7 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
   auto landed = [&](const Batch& b, uint32_t bar, uint32_t& phase) {
     if (b.valid != 0 && !dead) {
       dead = !__all_sync(0xffffffffu, pg_bar_wait(bar, phase));
-      phase ^= 1u;
+      if (!dead) phase ^= 1u;
     }
     __syncwarp();
   };
@@ -1124,48 +1136,48 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
       __syncwarp();
 #pragma unroll 1
       for (int a0 = 0; a0 < NQ; a0 += 4) {
-      float yy[4][E];                              // four rows at a time: their loads overlap
+        float yy[4][E];                              // four rows at a time: their loads overlap
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
+        for (int a = 0; a < 4; ++a) {
 #pragma unroll
-        for (int k = 0; k < E; ++k) yy[a][k] = 0.f;
-        if (a0 + a < p.group) pg_load_query<D>(p, bf, seq, head, a0 + a, lane, yy[a]);
-      }
+          for (int k = 0; k < E; ++k) yy[a][k] = 0.f;
+          if (a0 + a < p.group) pg_load_query<D>(p, bf, seq, head, a0 + a, lane, yy[a]);
+        }
 #pragma unroll
-      for (int a4 = 0; a4 < 4; ++a4) {
-        const int a = a0 + a4;
-        float (&y)[E] = yy[a4];
-        pg_turn_query<D>(p, lane, y);
-        if constexpr (EXACT) {
+        for (int a4 = 0; a4 < 4; ++a4) {
+          const int a = a0 + a4;
+          float (&y)[E] = yy[a4];
+          pg_turn_query<D>(p, lane, y);
+          if constexpr (EXACT) {
 #pragma unroll
-          for (int k = 0; k < E; k += 2) {         // pair (E lane + k) / 2
-            const int i = pair_slot<D>((E * lane + k) / 2);
-            *reinterpret_cast<float2*>(pw + C::W_Q + (a * 4 + i / KP) * C::QRUN + (i % KP) * 8) = make_float2(y[k], y[k + 1]);
-          }
-        } else {
-          // over the power of two that brings the largest element to [2^13, 2^14); then the fp16
-          // number next to each element and what is left, where the step that takes them loads them
-          float mx = 0.f;
+            for (int k = 0; k < E; k += 2) {         // pair (E lane + k) / 2
+              const int i = pair_slot<D>((E * lane + k) / 2);
+              *reinterpret_cast<float2*>(pw + C::W_Q + (a * 4 + i / KP) * C::QRUN + (i % KP) * 8) = make_float2(y[k], y[k + 1]);
+            }
+          } else {
+            // over the power of two that brings the largest element to [2^13, 2^14); then the fp16
+            // number next to each element and what is left, where the step that takes them loads them
+            float mx = 0.f;
 #pragma unroll
-          for (int k = 0; k < E; ++k) mx = fmaxf(mx, fabsf(y[k]));
+            for (int k = 0; k < E; ++k) mx = fmaxf(mx, fabsf(y[k]));
 #pragma unroll
-          for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-          const int ex = min(max(pg_exp_of(mx) - 13, -126), 126);
-          const float sc = pg_exp2i(-ex);
-          if (lane == 0) reinterpret_cast<float*>(pw + C::W_QS)[a] = pg_exp2i(ex);
+            for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const int ex = min(max(pg_exp_of(mx) - 13, -126), 126);
+            const float sc = pg_exp2i(-ex);
+            if (lane == 0) reinterpret_cast<float*>(pw + C::W_QS)[a] = pg_exp2i(ex);
 #pragma unroll
-          for (int k = 0; k < E; k += 2) {
-            const int i = pair_slot<D>((E * lane + k) / 2), r = i % KP;
-            const int at = BOOKS == kAnyBooks && p.k.nc <= 1 ? (r & ~7) + 2 * (r & 3) + ((r >> 2) & 1) : r;     // 4-bit norms: four apart
-            uint32_t* const w = reinterpret_cast<uint32_t*>(pw + C::W_Q) + (((at >> 2) * QT + (a >> 2)) * 32 + 8 * (a & 3) + i / KP) * 4 + (at & 3);
-            const float q0 = y[k] * sc, q1 = y[k + 1] * sc;
-            const __half2 hi = __floats2half2_rn(q0, q1);
-            const float2 back = __half22float2(hi);
-            w[0] = h2_bits(hi);
-            w[16] = h2_bits(__floats2half2_rn(q0 - back.x, q1 - back.y));
+            for (int k = 0; k < E; k += 2) {
+              const int i = pair_slot<D>((E * lane + k) / 2), r = i % KP;
+              const int at = BOOKS == kAnyBooks && p.k.nc <= 1 ? (r & ~7) + 2 * (r & 3) + ((r >> 2) & 1) : r;     // 4-bit norms: four apart
+              uint32_t* const w = reinterpret_cast<uint32_t*>(pw + C::W_Q) + (((at >> 2) * QT + (a >> 2)) * 32 + 8 * (a & 3) + i / KP) * 4 + (at & 3);
+              const float q0 = y[k] * sc, q1 = y[k + 1] * sc;
+              const __half2 hi = __floats2half2_rn(q0, q1);
+              const float2 back = __half22float2(hi);
+              w[0] = h2_bits(hi);
+              w[16] = h2_bits(__floats2half2_rn(q0 - back.x, q1 - back.y));
+            }
           }
         }
-      }
       }
       __syncwarp();
 #pragma unroll
@@ -1386,16 +1398,16 @@ __global__ void __launch_bounds__(Pg<D, QT, EXACT>::WARPS * 32, 1)
         for (int o = 4; o < 32; o <<= 1) l_[x] += __shfl_xor_sync(0xffffffffu, l_[x], o);
       if constexpr (EXACT) {
 #pragma unroll
-      for (int a = 0; a < NQ; ++a)
+        for (int a = 0; a < NQ; ++a)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 4; ++j) {
 #pragma unroll
-          for (int o = VL; o < 32; o <<= 1) {
-            acc[a][j].x += __shfl_xor_sync(0xffffffffu, acc[a][j].x, o);
-            acc[a][j].y += __shfl_xor_sync(0xffffffffu, acc[a][j].y, o);
+            for (int o = VL; o < 32; o <<= 1) {
+              acc[a][j].x += __shfl_xor_sync(0xffffffffu, acc[a][j].x, o);
+              acc[a][j].y += __shfl_xor_sync(0xffffffffu, acc[a][j].y, o);
+            }
+            if (vt == 0) *reinterpret_cast<float2*>(rec + a * pg_rec_floats(D) + 2 + 2 * slot_pair<D>(4 * vl + j)) = acc[a][j];
           }
-          if (vt == 0) *reinterpret_cast<float2*>(rec + a * pg_rec_floats(D) + 2 + 2 * slot_pair<D>(4 * vl + j)) = acc[a][j];
-        }
       } else {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {

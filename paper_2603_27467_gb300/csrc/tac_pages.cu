@@ -3,12 +3,18 @@
 // page_bounds: for each (page, head) that new rows touch, the channel-wise minimum and
 // maximum of its keys, rounded outward to whole numbers in [-127, 127] times the page's
 // power of two.  Minima, maxima and products with powers of two are exact, so the box does
-// not depend on the order of the rows or on how they came (one by one or as a prompt).
+// not depend on the order of the rows or on how they came (one by one or as a prompt).  Bound: HBM;
+// 67 MB of keys (512 pages of 64 rows, 8 heads, d = 128) take 13.2 us, 5.1 TB/s or 75 % of the measured
+// copy rate, 3 of them the wait for spans, table and first rows; a step's 2048 rows 5.7 us, launch and
+// those waits.
 //
 // select_pages: sum_j max(c_j lo_j, c_j hi_j) = sum_j min(c_j, 0) lo_j + max(c_j, 0) hi_j, one dot
 // product of 2 d whole numbers a query (mma.sync on fp16 numbers that hold them, exact); the powers
 // of two of the query and of the page come last, exact too.  (8-bit mma.sync is as exact and runs at
-// 128 products a cycle and SM here: 18.7 us for 8 x 8192 boxes against 13.)  So the order of the scores, and the pages that
+// 128 products a cycle and SM here: 18.7 us for 8 x 8192 boxes against 17.5.)  Bound: latency.  8 x 257
+// boxes take 7.4 us (lengths, table, boxes: three waits in a row, then the threshold's barriers), 256
+// (sequence, head)s of 16 to 512 boxes 10, 8 x 8192 18, of which scoring 8 (a warp's tiles one after
+// another) and the cluster's exchanges 5.  So the order of the scores, and the pages that
 // are chosen, are those of the definition, whatever the kernel's order of summation.
 #include <algorithm>
 #include <atomic>
@@ -245,7 +251,16 @@ static cudaError_t launch_bounds_t(const BoundsParams& p, int sms, cudaStream_t 
   const int64_t units = items * p.pg.heads;
   if (units < 1) return cudaSuccess;
   auto grid = [&](int upc) { return (unsigned)std::min<int64_t>((units + upc - 1) / upc, (int64_t)sms * 6); };
-  page_bounds_kernel<D, T, 1><<<grid(kPgWarps), kPgThreads, 0, st>>>(p);
+  // Long pages of few (page, head)s are shared by 2, 4 or 8 warps, at least 32 rows each, while that
+  // leaves no more than 32 warps an SM: 32 pages of 256 rows x 8 heads 14.3 -> 7.3 us, 128 such pages
+  // 15.4 -> 13.8; pages of 64 rows take longer shared (13.2 -> 16.2 us for 512 pages x 8 heads).
+  const int64_t rows = std::min<int64_t>(p.pg.page, p.rows / std::max(1, p.pg.seqs));
+  int split = 1;
+  while (split < 8 && rows >= 128 && rows / (2 * split) >= 32 && units * 2 * split <= (int64_t)sms * 32) split *= 2;
+  if (split == 8) page_bounds_kernel<D, T, 8><<<grid(kPgWarps / 8), kPgThreads, 0, st>>>(p);
+  else if (split == 4) page_bounds_kernel<D, T, 4><<<grid(kPgWarps / 4), kPgThreads, 0, st>>>(p);
+  else if (split == 2) page_bounds_kernel<D, T, 2><<<grid(kPgWarps / 2), kPgThreads, 0, st>>>(p);
+  else page_bounds_kernel<D, T, 1><<<grid(kPgWarps), kPgThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 

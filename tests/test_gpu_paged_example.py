@@ -75,3 +75,21 @@ def test_tables_of_many_sequences(tac_gpu, orc):
     sel = torch.tensor([[[0, 2, -1]]] * 300, dtype=torch.int32, device="cuda")
     cnt = torch.tensor([[s % 4] for s in range(300)], dtype=torch.int32, device="cuda")
     pages._check_attend(tac, orc, cache, table, lens, q, sel, cnt, rows=rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,rows,start", [(1, 2000, 0), (2, 255, 130), (2, 4096, 77), (16, 9000, 3)])
+def test_bounds_of_long_pages(tac_gpu, dtype, d, heads, rows, start):
+    """Pages of 256 and 1024 tokens, whose rows several warps share."""
+    import torch
+    tac = tac_gpu
+    import test_gpu_pages as pages
+    for page in (256, 1024):
+        table, count = pages._table([start + rows], page, 1, 3)
+        bounds = tac.PageBounds.empty(count, heads, d, page)
+        bounds.codes.fill_(5)
+        bounds.scales.fill_(0.5)
+        keys = (torch.randn((rows, heads, d), generator=pages._gen(rows), device="cuda") * 7).to(pages._dtype(dtype))
+        keys[rows // 2, 0, 3] = math.inf
+        pages._check_bounds(tac, keys, bounds, table, [start], [0, rows], page)
